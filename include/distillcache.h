@@ -471,6 +471,122 @@ dc_status dc_reinforce_terms(int32_t steps, int32_t rollouts, const dc_reinforce
                              double *returns_out, double *baseline_out, double *adv_out,
                              double *weight_out, double *stats_out, void *hip_stream);
 
+/* ---- Several tokens at once: prompts and drafted tokens -------------------
+ *
+ * The entry points above take one token per sequence and step.  These four put
+ * several at once into a cache, layer by layer as the model runs:
+ *   dc_qk_norm_rope      query and key heads normed and rotated; keys and values
+ *                        written behind the cache's rows
+ *   dc_prompt_attention  causal attention of a prompt (or its next part)
+ *   dc_tree_attention    attention of a tree of drafted tokens
+ *   dc_commit_rows       after the last layer: the rows, or an accepted path
+ *                        of them, become part of the cache
+ * Token r of a sequence belongs in slot rows + r of each of its units, rows being
+ * the unit's rows before the call (kv->len, or unit_len[u] clamped to [0, kv->len]).
+ * Until dc_commit_rows nothing but these entry points reads those slots, and a call that
+ * is not committed leaves the cache as it was (a decode step overwrites the slots).
+ * Both dtypes, ragged caches in float32 too (which dc_decode_step does not take).
+ * Model weights are frozen in this method: these are forward passes only.
+ */
+
+/* The tokens of one call, packed: those of sequence b are cu[b] .. cu[b + 1] - 1 of N.
+ * A sequence may have none.  Offsets on the device that are not ascending in
+ * [0, tokens], or counts over max_tokens, are clamped. */
+typedef struct {
+  int32_t tokens;       /* N, at least 1 */
+  int32_t max_tokens;   /* host: the most tokens of one sequence (1..tokens) */
+  const int32_t *cu;    /* device [batch + 1], or NULL: max_tokens each (tokens =
+                           batch * max_tokens) */
+} dc_tokens;
+
+/* Norm and rotation of a head x[head_dim], in float32 with one rounding at the end:
+ *   norm = 1: x <- x / sqrt(mean(x^2) + eps) * gain (NULL: ones); norm = 0: x as it is;
+ *   then pair i < rot_dim / 2 of its elements, (i, i + rot_dim / 2) or with interleaved
+ *   (2 i, 2 i + 1), turns by phi = position * inv_freq[i]:
+ *     (a, b) <- (a cos phi - b sin phi, a sin phi + b cos phi).
+ * The elements from rot_dim on are not turned.  phi is formed in binary64, so
+ * far positions keep their angle. */
+typedef struct {
+  int32_t norm;             /* 0 or 1 */
+  float eps;                /* finite, >= 0 */
+  const float *q_gain;      /* device [head_dim] or NULL */
+  const float *k_gain;      /* device [head_dim] or NULL */
+  int32_t rot_dim;          /* 0 (no rotation) or a multiple of 16 up to head_dim */
+  int32_t interleaved;      /* 0 or 1 */
+  const float *inv_freq;    /* device [rot_dim / 2] (NULL if rot_dim = 0) */
+} dc_rope;
+
+/* Norms and rotates the query and key heads of the tokens, for one layer.
+ *   q  [N][n_q_heads][head_dim], k [N][n_kv_heads][head_dim], v as k: token t at element
+ *      t * ld (ld >= heads * head_dim: parts of a fused projection are read in place)
+ *   pos    device [N] int32: the tokens' positions (NULL if rot_dim = 0)
+ *   q_out  [N][n_q_heads][head_dim] contiguous; may be q itself if ld_q = n_q_heads *
+ *          head_dim, and overlaps no input otherwise
+ *   k_out  NULL: the rotated keys and the values go to the slots behind the rows of
+ *          layer `layer` of kv; else [N][n_kv_heads][head_dim] contiguous (may be k
+ *          likewise), v and kv are not used and may be NULL: with q_out
+ *          the inputs of dc_decode_step for one token per sequence and one layer.
+ * Rows and pointers are multiples of 16 bytes.  dims.capacity >= kv->len + max_tokens.
+ * Errors: DC_ERR_NULL, DC_ERR_SHAPE (sizes, layer, ld), DC_ERR_CAPACITY, DC_ERR_VALUE
+ * (eps, flags), DC_ERR_UNSUPPORTED (rot_dim, alignment). */
+dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
+                          const dc_tokens *tokens, const dc_rope *rope, const void *q, int64_t ld_q,
+                          const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                          const int32_t *pos, void *q_out, void *k_out, void *hip_stream);
+
+/* Causal grouped-query attention of packed prompts over layer `layer` of the cache, whose
+ * slots behind the rows hold the tokens' own K/V (dc_qk_norm_rope): token r of a sequence
+ * sees the unit's rows and the tokens 0..r.
+ *   q    [N][n_q_heads][head_dim], dtype, contiguous
+ *   out  the same shape: o = sum_i a_i v_i, a = softmax_i(scale q.k_i); not q itself
+ * Slots that a token does not see have no influence on it, whatever they hold.
+ * Workspace: dc_tokens_workspace_bytes(dims, tokens, kv->len + max_tokens) bytes.
+ * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_CAPACITY, DC_ERR_WORKSPACE,
+ * DC_ERR_UNSUPPORTED (alignment, grids past 2^31 workgroups). */
+dc_status dc_prompt_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer,
+                              const dc_tokens *tokens, const void *q, void *out, void *ws,
+                              size_t ws_bytes, void *hip_stream);
+
+/* Most drafted tokens of one sequence. */
+#define DC_TREE_MAX_NODES 256
+
+/* Attention of drafted tokens, as dc_prompt_attention except for what they see: the unit's
+ * rows, themselves and their ancestors.
+ *   parent  device [N] int32: the node's parent, its number within the sequence, which
+ *           comes before it; a value that is no earlier node (-1) hangs the node
+ *           directly below the cache.  parent[r] = r - 1 is the causal prompt.
+ * Errors: those of dc_prompt_attention; DC_ERR_UNSUPPORTED also for max_tokens >
+ * DC_TREE_MAX_NODES. */
+dc_status dc_tree_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer,
+                            const dc_tokens *tokens, const int32_t *parent, const void *q, void *out,
+                            void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Workspace bytes of dc_prompt_attention and dc_tree_attention for tokens of these counts
+ * (tokens->cu is not read) and caches of up to max_len rows, the tokens' own included.
+ * 0 also for invalid sizes. */
+size_t dc_tokens_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, int32_t max_len);
+
+/* After all layers: the first rows behind the cache, or an accepted path of them, become
+ * part of every unit.
+ *   width  the most rows that a sequence keeps (1..max_tokens)
+ *   path   device [batch][width] int32 or NULL.  Row j of sequence b is the one of its token
+ *          path[b][j] (ascending; an entry below j counts as j, one past the sequence's
+ *          tokens as its last); NULL: of token j.  max_tokens <= DC_TREE_MAX_NODES.
+ *   keep   device [batch] int32 or NULL: rows that sequence b keeps, clamped to
+ *          [0, min(width, its tokens)]; NULL: all of them.
+ *   feat   NULL (a teacher cache) or the feature state, which gets the rows as
+ *          dc_feat_init would: alpha = ent_num = ent_den = sigma = 0, vnorm, and positions
+ *          next_pos + j.
+ * K and V of the path move in place.  Afterwards unit_len[u] += rows kept, kv->len +=
+ * width, feat->next_pos += width (host: the caller may lower kv->len to any bound of the
+ * unit lengths that it knows, and next_pos to any value past the positions in use).
+ * Equal counts need nothing else; cu or keep make the units' lengths differ, which
+ * takes a ragged cache.
+ * Errors: DC_ERR_NULL (dims, kv, tokens, buffers; cu or keep without kv->unit_len),
+ * DC_ERR_SHAPE, DC_ERR_CAPACITY (kv->len + max_tokens > capacity), DC_ERR_UNSUPPORTED. */
+dc_status dc_commit_rows(const dc_dims *dims, dc_kv *kv, dc_feat *feat, const dc_tokens *tokens,
+                         const int32_t *path, const int32_t *keep, int32_t width, void *hip_stream);
+
 /* Static string naming a status. */
 const char *dc_status_str(dc_status s);
 

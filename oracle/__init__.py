@@ -22,6 +22,8 @@ Every value is computed in binary64 from the exact stored input values
   log-partition log Z(s, B, tau) and log pi(a | s) (Sec. 3.1.2, App. C).
 * ``reinforce``  – rollout reward math of the REINFORCE update: discounted
   returns, RLOO and EMA baselines, entropy surrogate, loss (Sec. 3.2).
+* ``prompt``     – several tokens at once: norm and rotation of heads, attention of
+  prompts and of trees of drafted tokens, the rows an accepted path keeps.
 * ``unit``       – one unit's cache and feature state stepped through
   append -> attention -> features -> score -> select -> prune (Algorithm 1,
   Sec. 3.1.3 for the student/teacher caches).

@@ -57,6 +57,17 @@ class dc_reinforce_cfg(ctypes.Structure):
     _fields_ = [("gamma", ctypes.c_double), ("beta", ctypes.c_double), ("ema_decay", ctypes.c_double)]
 
 
+class dc_tokens(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("cu", ctypes.c_void_p)]
+
+
+class dc_rope(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_int32), ("eps", ctypes.c_float), ("q_gain", ctypes.c_void_p),
+                ("k_gain", ctypes.c_void_p), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p)]
+
+
+TREE_MAX_NODES = 256
 KL_MAX_ROWS = 16384
 KL_STATIC_MAX_PAIRS = 524288     # rows * (vocab / 64) of one dc_kl_reward_static call
 
@@ -68,7 +79,8 @@ EXPORTS = ("dc_workspace_bytes", "dc_feat_init", "dc_decode_step", "dc_score_evi
            "dc_kl_reward_packed", "dc_kl_reward_static",
            "dc_reinforce_terms",
            "dc_dynamic_budget", "dc_global_alpha", "dc_global_alpha_workspace_bytes",
-           "dc_status_str")
+           "dc_qk_norm_rope", "dc_prompt_attention", "dc_tree_attention", "dc_commit_rows",
+           "dc_tokens_workspace_bytes", "dc_status_str")
 
 _lib = None
 
@@ -137,6 +149,23 @@ def lib() -> ctypes.CDLL:
         L.dc_global_alpha_workspace_bytes.restype = sz
         L.dc_dynamic_budget.argtypes = [ctypes.c_float, i32, i32]
         L.dc_dynamic_budget.restype = i32
+        i64 = ctypes.c_int64
+        L.dc_qk_norm_rope.argtypes = [ctypes.POINTER(dc_dims), ctypes.POINTER(dc_kv), i32,
+                                      ctypes.POINTER(dc_tokens), ctypes.POINTER(dc_rope), vp, i64,
+                                      vp, i64, vp, i64, vp, vp, vp, vp]
+        L.dc_qk_norm_rope.restype = ctypes.c_int
+        L.dc_prompt_attention.argtypes = [ctypes.POINTER(dc_dims), ctypes.POINTER(dc_kv), i32,
+                                          ctypes.POINTER(dc_tokens), vp, vp, vp, sz, vp]
+        L.dc_prompt_attention.restype = ctypes.c_int
+        L.dc_tree_attention.argtypes = [ctypes.POINTER(dc_dims), ctypes.POINTER(dc_kv), i32,
+                                        ctypes.POINTER(dc_tokens), vp, vp, vp, vp, sz, vp]
+        L.dc_tree_attention.restype = ctypes.c_int
+        L.dc_commit_rows.argtypes = [ctypes.POINTER(dc_dims), ctypes.POINTER(dc_kv),
+                                     ctypes.POINTER(dc_feat), ctypes.POINTER(dc_tokens), vp, vp, i32,
+                                     vp]
+        L.dc_commit_rows.restype = ctypes.c_int
+        L.dc_tokens_workspace_bytes.argtypes = [ctypes.POINTER(dc_dims), ctypes.POINTER(dc_tokens), i32]
+        L.dc_tokens_workspace_bytes.restype = sz
         L.dc_status_str.argtypes = [ctypes.c_int]
         L.dc_status_str.restype = ctypes.c_char_p
         _lib = L
@@ -284,3 +313,31 @@ def dc_score_evict_units(dims, kv, feat, policy, budgets, max_budget: int, gumbe
     _check(lib().dc_score_evict_units(ctypes.byref(dims), ctypes.byref(kv), _ref(feat), _ref(policy),
                                       _ptr(budgets), max_budget, _ref(gumbel), _ptr(scores_out),
                                       _ptr(kept_out), _ptr(logp_out), _ptr(ws), ws_bytes, stream))
+
+
+def dc_qk_norm_rope(dims, kv, layer: int, tokens, rope, q, ld_q: int, k, ld_k: int, v, ld_v: int, pos,
+                    q_out, k_out=None, stream=None) -> None:
+    _check(lib().dc_qk_norm_rope(ctypes.byref(dims), _ref(kv), layer, ctypes.byref(tokens),
+                                 ctypes.byref(rope), _ptr(q), ld_q, _ptr(k), ld_k, _ptr(v), ld_v,
+                                 _ptr(pos), _ptr(q_out), _ptr(k_out), stream))
+
+
+def dc_prompt_attention(dims, kv, layer: int, tokens, q, out, ws=None, ws_bytes: int = 0,
+                        stream=None) -> None:
+    _check(lib().dc_prompt_attention(ctypes.byref(dims), ctypes.byref(kv), layer, ctypes.byref(tokens),
+                                     _ptr(q), _ptr(out), _ptr(ws), ws_bytes, stream))
+
+
+def dc_tree_attention(dims, kv, layer: int, tokens, parent, q, out, ws=None, ws_bytes: int = 0,
+                      stream=None) -> None:
+    _check(lib().dc_tree_attention(ctypes.byref(dims), ctypes.byref(kv), layer, ctypes.byref(tokens),
+                                   _ptr(parent), _ptr(q), _ptr(out), _ptr(ws), ws_bytes, stream))
+
+
+def dc_tokens_workspace_bytes(dims, tokens, max_len: int) -> int:
+    return int(lib().dc_tokens_workspace_bytes(ctypes.byref(dims), ctypes.byref(tokens), max_len))
+
+
+def dc_commit_rows(dims, kv, feat, tokens, path=None, keep=None, width: int = 0, stream=None) -> None:
+    _check(lib().dc_commit_rows(ctypes.byref(dims), ctypes.byref(kv), _ref(feat), ctypes.byref(tokens),
+                                _ptr(path), _ptr(keep), width, stream))

@@ -2,6 +2,7 @@
 streams only; no computation happens here)."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -64,6 +65,7 @@ class DecodeBuffers:
                 self.feat.sigma = self.sigma.data_ptr()
         self.ws = None
         self.ws_bytes = 0
+        self._older_ws = []
         if features:
             self.reserve_workspace(capacity)
 
@@ -176,6 +178,154 @@ class DecodeBuffers:
                      stream=None):
         B.dc_sample_evict(self.dims, self.kv, self.feat, policy, budget, gumbel, scores_out,
                           kept_out, logp_out, self.ws, self.ws_bytes, stream_handle(stream))
+
+
+    # ---- several tokens at once: prompts and drafted tokens
+
+    def _rows_of(self, x, heads, tokens, name):
+        """x [N][heads][d] with dense rows: its elements from token to token."""
+        self._batch_of(tokens)
+        if x.dtype != self.k.dtype or tuple(x.shape) != (tokens.tokens, heads, self.D):
+            raise ValueError(f"{name} must be {self.k.dtype} [{tokens.tokens}][{heads}][{self.D}], "
+                             f"got {x.dtype} {list(x.shape)}")
+        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.D):
+            raise ValueError(f"{name}'s heads must be contiguous within a token")
+        self._here(x, name)
+        # (a single token's stride is never used)
+        return x.stride(0) if tokens.tokens > 1 else heads * self.D
+
+    def _batch_of(self, tokens):
+        n = getattr(tokens, "sequences", self.dims.batch)
+        if n != self.dims.batch:
+            raise ValueError(f"tokens of {n} sequences for a cache of {self.dims.batch}")
+
+    def _here(self, x, name):
+        if x.device != self.k.device:
+            raise ValueError(f"{name} is on {x.device}, the cache on {self.k.device}")
+
+    def _stream_here(self, stream):
+        """The stream's handle; the cache has to be on the current device, which launches it."""
+        if self.k.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache is on {self.k.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+        return stream_handle(stream)
+
+    def _empty(self, shape, dtype, stream):
+        """Memory that the given stream uses first (the allocator orders reuse by stream)."""
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.k.device)
+
+    def _ints(self, x, shape, name):
+        if x is not None and (x.dtype != torch.int32 or tuple(x.shape) != shape or not x.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous int32 {list(shape)}, got {x.dtype} {list(x.shape)}")
+        if x is not None:
+            self._here(x, name)
+
+    def norm_rope(self, tokens, rope, q, k, v=None, pos=None, layer=0, q_out=None, k_out=None, stream=None):
+        """Queries and keys of `tokens` normed and rotated (dc_qk_norm_rope).  With v the rotated
+        keys and the values go into the cache behind its rows; without, the keys are
+        returned too.  Returns (q_out, k_out or None)."""
+        hq, hk = self.dims.n_q_heads, self.dims.n_kv_heads
+        ld_q, ld_k = self._rows_of(q, hq, tokens, "q"), self._rows_of(k, hk, tokens, "k")
+        ld_v = self._rows_of(v, hk, tokens, "v") if v is not None else 0
+        self._ints(pos, (tokens.tokens,), "pos")
+        if q_out is None:
+            q_out = self._empty((tokens.tokens, hq, self.D), q.dtype, stream)
+        elif not q_out.is_contiguous() or q_out.shape != q.shape or q_out.dtype != q.dtype:
+            raise ValueError("q_out must be contiguous and like q")
+        if v is not None:
+            if k_out is not None:
+                raise ValueError("with v the keys go to the cache: no k_out")
+        elif k_out is None:
+            k_out = self._empty((tokens.tokens, hk, self.D), k.dtype, stream)
+        elif not k_out.is_contiguous() or k_out.shape != k.shape or k_out.dtype != k.dtype:
+            raise ValueError("k_out must be contiguous and like k")
+        B.dc_qk_norm_rope(self.dims, self.kv, layer, tokens, rope, q, ld_q, k, ld_k, v, ld_v, pos, q_out, k_out,
+                          self._stream_here(stream))
+        return q_out, k_out
+
+    def _tokens_workspace(self, tokens, stream):
+        need = B.dc_tokens_workspace_bytes(self.dims, tokens, self.kv.len + tokens.max_tokens)
+        if need > self.ws_bytes:
+            self._older_ws.append(self.ws)       # a captured graph may hold its address
+            self.ws = self._empty(need, torch.uint8, stream)
+            self.ws_bytes = need
+
+    def _check_queries(self, tokens, q, out, stream):
+        self._rows_of(q, self.dims.n_q_heads, tokens, "q")
+        if not q.is_contiguous():
+            raise ValueError("q must be contiguous")
+        if out is None:
+            return self._empty(q.shape, q.dtype, stream)
+        if not out.is_contiguous() or out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out must be contiguous and like q")
+        return out
+
+    def prompt_attention(self, tokens, q, layer=0, out=None, stream=None):
+        """Causal attention of packed prompts whose K/V are behind the cache's rows."""
+        out = self._check_queries(tokens, q, out, stream)
+        self._tokens_workspace(tokens, stream)
+        B.dc_prompt_attention(self.dims, self.kv, layer, tokens, q, out, self.ws, self.ws_bytes,
+                              self._stream_here(stream))
+        return out
+
+    def tree_attention(self, tokens, parent, q, layer=0, out=None, stream=None):
+        """Attention of drafted tokens over the cache, themselves and their ancestors."""
+        out = self._check_queries(tokens, q, out, stream)
+        self._ints(parent, (tokens.tokens,), "parent")
+        self._tokens_workspace(tokens, stream)
+        B.dc_tree_attention(self.dims, self.kv, layer, tokens, parent, q, out, self.ws, self.ws_bytes,
+                            self._stream_here(stream))
+        return out
+
+    def commit_rows(self, tokens, path=None, keep=None, width=None, stream=None):
+        """The rows of `tokens`, or of each sequence's `path` [batch][width], join the cache."""
+        self._batch_of(tokens)
+        if path is not None:
+            width = path.shape[1] if path.dim() == 2 else 0
+            self._ints(path, (self.dims.batch, width), "path")
+        elif width is None:
+            width = tokens.max_tokens
+        self._ints(keep, (self.dims.batch,), "keep")
+        B.dc_commit_rows(self.dims, self.kv, self.feat, tokens, path, keep, width, self._stream_here(stream))
+
+    def prefill(self, tokens, rope, q, k, v, pos, layer=0, out=None, stream=None):
+        """One layer of a prompt: norm, rotation, the rows into the cache, attention.  After
+        the last layer commit_rows(tokens) makes the rows part of the cache."""
+        q, _ = self.norm_rope(tokens, rope, q, k, v, pos, layer, stream=stream)
+        return self.prompt_attention(tokens, q, layer, out, stream)
+
+    def draft(self, tokens, parent, rope, q, k, v, pos, layer=0, out=None, stream=None):
+        """One layer of a tree of drafted tokens: norm, rotation, the rows behind the cache,
+        attention.  commit_rows(tokens, path, keep) then keeps the accepted path."""
+        q, _ = self.norm_rope(tokens, rope, q, k, v, pos, layer, stream=stream)
+        return self.tree_attention(tokens, parent, q, layer, out, stream)
+
+
+def make_tokens(counts, device="cuda") -> B.dc_tokens:
+    """Packed tokens of sequences of `counts` (host) tokens each."""
+    counts = [int(c) for c in counts]
+    most, total = max(counts), sum(counts)
+    t = B.dc_tokens(total, most, None)
+    t.sequences = len(counts)
+    if min(counts) < most:
+        cu = [0]
+        for c in counts:
+            cu.append(cu[-1] + c)
+        t.cu_tensor = torch.tensor(cu, dtype=torch.int32, device=device)   # kept alive with t
+        t.cu = t.cu_tensor.data_ptr()
+    return t
+
+
+def make_rope(inv_freq=None, interleaved=False, norm=False, eps=1e-6, q_gain=None, k_gain=None) -> B.dc_rope:
+    """Norm and rotation of a head; inv_freq [rot_dim / 2] float32 on the device (None: no rotation)."""
+    for name, x in (("inv_freq", inv_freq), ("q_gain", q_gain), ("k_gain", k_gain)):
+        if x is not None and (x.dtype != torch.float32 or x.dim() != 1 or not x.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 vector")
+    r = B.dc_rope(int(norm), eps, B._ptr(q_gain), B._ptr(k_gain),
+                  0 if inv_freq is None else 2 * inv_freq.numel(), int(interleaved), B._ptr(inv_freq))
+    r.tensors = (inv_freq, q_gain, k_gain)       # kept alive with r
+    return r
 
 
 def subset_log_prob(scores: torch.Tensor, budget: int, tau: float = 1.0, kept=None, logz=True,

@@ -824,3 +824,203 @@ dc_status dc_kl_reward_static(int32_t rows, int32_t hidden, int32_t vocab, const
 }
 
 }  // extern "C"
+
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+dc_status check_tokens(const dc_dims* dims, const dc_tokens* t) {
+  const dc_status st = check_dims(dims);
+  if (st != DC_OK) return st;
+  if (!t) return DC_ERR_NULL;
+  if (t->tokens < 1 || t->max_tokens < 1 || t->max_tokens > t->tokens) return DC_ERR_SHAPE;
+  const int64_t most = (int64_t)dims->batch * t->max_tokens;
+  if (t->cu ? t->tokens > most : t->tokens != most) return DC_ERR_SHAPE;
+  return DC_OK;
+}
+
+// The slots behind the rows of one layer of the cache.
+dc_status check_rows(const dc_dims* dims, const dc_kv* kv, const dc_tokens* t) {
+  if (!kv || !kv->k || !kv->v) return DC_ERR_NULL;
+  if (kv->len < 0 || kv->len > dims->capacity) return DC_ERR_SHAPE;
+  if (t->max_tokens > dims->capacity - kv->len) return DC_ERR_CAPACITY;
+  if (!aligned16(kv->k) || !aligned16(kv->v)) return DC_ERR_UNSUPPORTED;
+  return DC_OK;
+}
+
+dc::TokenArgs token_args(const dc_tokens* t) { return dc::TokenArgs{t->cu, t->tokens, t->max_tokens}; }
+
+int log2_of(int g) { return g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3; }
+
+// Sizes of an attention call and how it is cut, for caches of up to L rows; the workspace it needs.
+bool plan_attend(const dc_dims* dims, const dc_tokens* t, int L, dc::AttendArgs& a, size_t& need) {
+  memset(&a, 0, sizeof(a));
+  a.tok = token_args(t);
+  a.batch = dims->batch;
+  a.n_layers = dims->n_layers;
+  a.hq = dims->n_q_heads;
+  a.hk = dims->n_kv_heads;
+  a.gshift = log2_of(group_of(dims));
+  a.cap = dims->capacity;
+  a.scale = scale_of(dims);
+  const bool ok = dc::attend_plan(a, dims->dtype, dims->head_dim, L);
+  need = a.splits > 1 ? align256((size_t)t->tokens * a.hq * a.splits * (dims->head_dim + 2) * sizeof(float)) : 0;
+  return ok;
+}
+
+dc_status attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens,
+                 const int32_t* parent, const void* q, void* out, void* ws, size_t ws_bytes,
+                 void* hip_stream) {
+  dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  if (!q || !out) return DC_ERR_NULL;
+  if (layer < 0 || layer >= dims->n_layers) return DC_ERR_SHAPE;
+  st = check_rows(dims, kv, tokens);
+  if (st != DC_OK) return st;
+  if (!aligned16(q) || !aligned16(out) || q == out) return DC_ERR_UNSUPPORTED;
+  dc::AttendArgs a;
+  size_t need = 0;
+  if (!plan_attend(dims, tokens, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
+  if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
+  if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  a.q = q;
+  a.out = out;
+  a.k = kv->k;
+  a.v = kv->v;
+  a.unit_len = kv->unit_len;
+  a.parent = parent;
+  a.part = need ? (float*)ws : nullptr;
+  a.layer = layer;
+  a.len = kv->len;
+  return dc::launch_attend(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+dc_status dc_qk_norm_rope(const dc_dims* dims, const dc_kv* kv, int32_t layer,
+                          const dc_tokens* tokens, const dc_rope* rope, const void* q, int64_t ld_q,
+                          const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                          const int32_t* pos, void* q_out, void* k_out, void* hip_stream) {
+  dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  const bool cache = k_out == nullptr;
+  if (!rope || !q || !k || !q_out || (cache && !v)) return DC_ERR_NULL;
+  if (rope->rot_dim != 0 && (!rope->inv_freq || !pos)) return DC_ERR_NULL;
+  if ((rope->norm != 0 && rope->norm != 1) || (rope->interleaved != 0 && rope->interleaved != 1) ||
+      !(rope->eps >= 0.0f) || isinf(rope->eps))
+    return DC_ERR_VALUE;
+  if (rope->rot_dim < 0 || rope->rot_dim > dims->head_dim) return DC_ERR_SHAPE;
+  if (rope->rot_dim % 16) return DC_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= dims->n_layers) return DC_ERR_SHAPE;
+  const int64_t wq = (int64_t)dims->n_q_heads * dims->head_dim, wk = (int64_t)dims->n_kv_heads * dims->head_dim;
+  if (ld_q < wq || ld_k < wk || (cache && ld_v < wk)) return DC_ERR_SHAPE;
+  if (cache) {
+    st = check_rows(dims, kv, tokens);
+    if (st != DC_OK) return st;
+  }
+  const int per16 = dims->dtype == DC_BF16 ? 8 : 4;
+  if (ld_q % per16 || ld_k % per16 || (cache && ld_v % per16) || !aligned16(q) || !aligned16(k) ||
+      !aligned16(q_out) || !aligned16(cache ? v : k_out))
+    return DC_ERR_UNSUPPORTED;
+  if ((q == q_out && ld_q != wq) || (!cache && k == k_out && ld_k != wk)) return DC_ERR_UNSUPPORTED;
+  dc::NormRopeArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_v = ld_v;
+  a.pos = pos;
+  a.q_gain = rope->q_gain;
+  a.k_gain = rope->k_gain;
+  a.inv_freq = rope->inv_freq;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  if (cache) {
+    a.kc = kv->k;
+    a.vc = kv->v;
+    a.unit_len = kv->unit_len;
+    a.len = kv->len;
+  }
+  a.cap = dims->capacity;
+  a.tok = token_args(tokens);
+  a.batch = dims->batch;
+  a.n_layers = dims->n_layers;
+  a.layer = layer;
+  a.hq = dims->n_q_heads;
+  a.hk = dims->n_kv_heads;
+  a.norm = rope->norm;
+  a.rot = rope->rot_dim;
+  a.interleaved = rope->interleaved;
+  a.eps = rope->eps;
+  return dc::launch_norm_rope(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
+}
+
+dc_status dc_prompt_attention(const dc_dims* dims, const dc_kv* kv, int32_t layer,
+                              const dc_tokens* tokens, const void* q, void* out, void* ws,
+                              size_t ws_bytes, void* hip_stream) {
+  return attend(dims, kv, layer, tokens, nullptr, q, out, ws, ws_bytes, hip_stream);
+}
+
+dc_status dc_tree_attention(const dc_dims* dims, const dc_kv* kv, int32_t layer,
+                            const dc_tokens* tokens, const int32_t* parent, const void* q, void* out,
+                            void* ws, size_t ws_bytes, void* hip_stream) {
+  const dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  if (!parent) return DC_ERR_NULL;
+  if (tokens->max_tokens > DC_TREE_MAX_NODES) return DC_ERR_UNSUPPORTED;
+  return attend(dims, kv, layer, tokens, parent, q, out, ws, ws_bytes, hip_stream);
+}
+
+size_t dc_tokens_workspace_bytes(const dc_dims* dims, const dc_tokens* tokens, int32_t max_len) {
+  if (check_tokens(dims, tokens) != DC_OK || max_len < 1) return 0;
+  dc::AttendArgs a;
+  size_t need = 0;
+  return plan_attend(dims, tokens, max_len, a, need) ? need : 0;
+}
+
+dc_status dc_commit_rows(const dc_dims* dims, dc_kv* kv, dc_feat* feat, const dc_tokens* tokens,
+                         const int32_t* path, const int32_t* keep, int32_t width, void* hip_stream) {
+  dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  st = check_rows(dims, kv, tokens);
+  if (st != DC_OK) return st;
+  if (feat) {
+    if (!feat->alpha || !feat->ent_num || !feat->ent_den || !feat->pos || !feat->vnorm) return DC_ERR_NULL;
+    if (feat->next_pos < 0 || feat->next_pos > INT32_MAX - tokens->max_tokens) return DC_ERR_SHAPE;
+  }
+  if ((tokens->cu || keep) && !kv->unit_len) return DC_ERR_NULL;
+  if (width < 1 || width > tokens->max_tokens) return DC_ERR_SHAPE;
+  if (path && tokens->max_tokens > DC_TREE_MAX_NODES) return DC_ERR_UNSUPPORTED;
+  dc::CommitArgs a;
+  memset(&a, 0, sizeof(a));
+  a.k = kv->k;
+  a.v = kv->v;
+  if (feat) {
+    a.alpha = feat->alpha;
+    a.num = feat->ent_num;
+    a.den = feat->ent_den;
+    a.pos = feat->pos;
+    a.vnorm = feat->vnorm;
+    a.sigma = feat->sigma;
+    a.next_pos = feat->next_pos;
+  }
+  a.unit_len = kv->unit_len;
+  a.path = path;
+  a.keep = keep;
+  a.cap = dims->capacity;
+  a.tok = token_args(tokens);
+  a.units = (int)units_of(dims);
+  a.per_seq = dims->n_layers * dims->n_kv_heads;
+  a.len = kv->len;
+  a.width = width;
+  if (dc::launch_commit(a, dims->dtype, dims->head_dim, hip_stream) != 0) return DC_ERR_HIP;
+  kv->len += width;
+  if (feat) feat->next_pos += width;
+  return DC_OK;
+}
+
+}  // extern "C"

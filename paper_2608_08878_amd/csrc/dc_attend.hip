@@ -1,0 +1,539 @@
+// Attention of several new tokens per sequence over cache rows, on gfx950 matrix cores:
+// a prompt (or its next chunk), causal, or a tree of drafted tokens.  The tokens' own K/V
+// rows are in the cache already, behind the rows that were there (slots len_u + r).
+//
+//   o = sum_i a_i v_i,  a = softmax_i(scale q.k_i)  over the rows i that the token sees:
+// every row below len_u, and of the tokens' own row len_u + r' for r' <= r (prompt) or for r' = r
+// and the ancestors of r (tree).
+//
+// A row here is a (token, query head) pair of one KV head, token-major (row = token G + j), so the
+// G heads that share K/V share its tiles.  A wave owns 32 rows and walks key tiles with a running
+// maximum and sum.  It computes S^T = K Q^T with 32x32 MFMAs: the accumulator then holds 16 keys
+// of one row per lane, so the softmax is lane-local but for one exchange between the wave's halves,
+// and the same registers are the right operand of O^T += V^T P^T without any movement, the key
+// order of the sum being free as long as V is read in the same one.  K and V tiles go from memory
+// to LDS directly (their 16-byte chunks permuted at the source so that operand reads spread over the
+// banks); bf16 V is read through the transposing LDS load.
+#include "dc_device.hpp"
+#include "dc_kernels.hpp"
+#include "distillcache.h"
+
+#pragma clang fp contract(off)
+
+namespace dc {
+
+namespace {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x8_t __attribute__((ext_vector_type(8)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef short i16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_c_t;
+
+constexpr int MAX_NODES = DC_TREE_MAX_NODES;
+constexpr int MASK_WORDS = MAX_NODES / 32;
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+// Rows of K and V in LDS.  Chunk c (16 bytes) of row r sits at position c ^ kx(r), c ^ vx(r).
+template <int DT, int D>
+struct KVT {
+  static constexpr int E = DT == 0 ? 4 : 2;
+  static constexpr int RB = D * E;            // bytes of a row
+  static constexpr int CH = RB / 16;          // chunks of a row
+  static constexpr int KT = CH / 2;           // 16-byte operand steps of a dot product
+  // K: 32 lanes read the same chunk of 32 rows; 16 bank groups of 16 bytes
+  __device__ static __forceinline__ int kx(int r) { return r & (CH < 16 ? CH - 1 : 15); }
+  // V, bf16: 16 lanes read 32 bytes of each of 4 rows; f32: 32 lanes read 128 bytes of row r,
+  // the others of row r + 4
+  __device__ static __forceinline__ int vx(int r) {
+    if constexpr (DT == 0) return 8 * ((r >> 2) & 1);
+    return CH == 16 ? 4 * (r & 3) : 4 * ((r >> 1) & 1);
+  }
+};
+
+__device__ __forceinline__ float half_max(float x) {   // over the wave's two halves
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+  return (uint32_t)(uintptr_t)(lds_c_t*)p;
+}
+
+// Factor of sums taken against the maximum m when the maximum becomes mn.  Maxima are kept as
+// fl(scale log2(e) max s), the number that the exponents subtract, so that its rounding is the
+// same in every term of a row and cancels.
+__device__ __forceinline__ float rescale(float m, float mn) {
+  return m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+}
+
+// Key held by accumulator register i of a lane in half h of the wave: bit i of a 32-key block.
+__device__ __forceinline__ int key_of(int i, int h) { return 8 * (i / 4) + 4 * h + i % 4; }
+
+// S^T of 32 keys (LDS rows kr .. kr + 31 at k) and the wave's 32 rows.
+template <int DT, int D>
+__device__ __forceinline__ f32x16_t scores32(const char* k, const uint4* qf, int lane) {
+  using T = KVT<DT, D>;
+  const int r = lane & 31, h = lane >> 5;
+  const char* row = k + r * T::RB;
+  f32x16_t s = {};
+#pragma unroll
+  for (int t = 0; t < T::KT; ++t) {
+    const uint4 kf = *reinterpret_cast<const uint4*>(row + ((2 * t + h) ^ T::kx(r)) * 16);
+    if constexpr (DT == 1) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf),
+                                                  __builtin_bit_cast(bf16x8_t, qf[t]), s, 0, 0, 0);
+    } else {
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.x), __uint_as_float(qf[t].x), s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.y), __uint_as_float(qf[t].y), s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.z), __uint_as_float(qf[t].z), s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.w), __uint_as_float(qf[t].w), s, 0, 0, 0);
+    }
+  }
+  return s;
+}
+
+// O^T += V^T P^T over 32 keys.  p[i] is the weight of key key_of(i, h).  bf16: the weights are
+// rounded to bf16 (half a step, 2^-9 of each), as the matrix cores take them; their sum l is of the
+// unrounded ones.
+template <int DT, int D>
+__device__ __forceinline__ void values32(const char* v, const f32x16_t& p, f32x16_t* o, int lane) {
+  using T = KVT<DT, D>;
+  const int h = lane >> 5;
+  if constexpr (DT == 1) {
+    const int i = lane & 15, dsub = (lane >> 4) & 1;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      f32x8_t pf;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pf[j] = p[8 * s + j];
+      const bf16x8_t pb = __builtin_convertvector(pf, bf16x8_t);
+      const int r0 = 16 * s + 4 * h + i / 4, r1 = r0 + 8;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const int c = 4 * db + 2 * dsub + (i & 3) / 2, off = (i & 1) * 8;
+        const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) i16x4_t*)(v + r0 * T::RB + (c ^ T::vx(r0)) * 16 + off));
+        const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) i16x4_t*)(v + r1 * T::RB + (c ^ T::vx(r1)) * 16 + off));
+        const i16x8_t vf = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), pb, o[db], 0, 0, 0);
+      }
+    }
+  } else {
+    const int dl = lane & 31;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = key_of(i, h);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const int c = 8 * db + dl / 4;
+        const float vf = *reinterpret_cast<const float*>(v + r * T::RB + (c ^ T::vx(r)) * 16 + (dl & 3) * 4);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p[i], o[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// The same sum key by key, leaving out the keys whose bit in `sees` is clear: a masked value row
+// that is infinite or NaN reaches no row that does not see it (0 times it is NaN).
+template <int DT, int D>
+__device__ __forceinline__ void values32_masked(const char* v, const f32x16_t& p, uint32_t sees, f32x16_t* o,
+                                             int lane) {
+  using T = KVT<DT, D>;
+  const int h = lane >> 5;
+  for (int kk = 0; kk < 32; ++kk) {
+    float w = 0.0f;
+    const int i = 4 * (kk / 8) + kk % 4, hk = (kk >> 2) & 1;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) w = i == x ? p[x] : w;
+    w = __shfl(w, (lane & 31) + 32 * hk);
+    if constexpr (DT == 1) w = __builtin_bit_cast(float, (uint32_t)f32_to_bf16_bits(w) << 16);
+    const bool on = (sees >> kk) & 1;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int d = 32 * db + key_of(x, h);
+        const char* at = v + kk * T::RB + ((d * T::E / 16) ^ T::vx(kk)) * 16 + (d * T::E) % 16;
+        float vf;
+        if constexpr (DT == 1) vf = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
+        else vf = *reinterpret_cast<const float*>(at);
+        if (on) o[db][x] = __builtin_fmaf(w, vf, o[db][x]);
+      }
+  }
+}
+
+// Row tiles of 32 RW rows; the key tile of SK KW keys is shared by the RW row waves, or cut among
+// KW groups of them, whose partial results are joined at the end.
+template <int DT, int D, int RW, int KW, int SK>
+struct Cfg {
+  static constexpr int NW = RW * KW, THREADS = 64 * NW, BM = 32 * RW, BN = SK * KW;
+  static constexpr int TILE = BN * KVT<DT, D>::RB;        // bytes of a K (or V) tile
+  static constexpr int BUF = 2 * TILE;
+  static constexpr int OB = 32 * D * 4 + 256;             // one wave's partial result
+  static constexpr int LDS = 2 * BUF;
+  static_assert((KW - 1) * RW * OB <= LDS, "partials fit the tile buffers");
+  static_assert(TILE % 1024 == 0 && SK % 32 == 0, "tile shape");
+};
+
+template <int DT, int D, int RW, int KW, int SK, bool TREE>
+__global__ void __launch_bounds__(64 * RW * KW) attend_kernel(AttendArgs a) {
+  using T = KVT<DT, D>;
+  using C = Cfg<DT, D, RW, KW, SK>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  __shared__ uint32_t anc[TREE ? MAX_NODES * MASK_WORDS : 1];
+  __shared__ int up[TREE ? MAX_NODES : 1];
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = wave % RW, kw = wave / RW;
+  const int G = 1 << a.gshift;
+
+  // One launch index per (row tile, key part, sequence and KV head), the pairs fastest: with a
+  // multiple of 8 of them a pair's workgroups share one XCD's L2.  The tiles with the most keys
+  // go first.
+  const int pairs = a.batch * a.hk;
+  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int split = rest % a.splits, tile = a.ntiles - 1 - rest / a.splits;
+  const int b = pair / a.hk, g = pair % a.hk;
+  const int u = (b * a.n_layers + a.layer) * a.hk + g;
+  int t0, n;
+  token_range(a.tok, b, t0, n);
+  const int rows = n << a.gshift, row0 = tile * C::BM;
+  if (row0 >= rows) return;
+  const int start = rows_before(a.unit_len, a.len, u), total = start + n;
+  const int last = (row0 + C::BM < rows ? row0 + C::BM : rows) - 1;
+  const int kend = TREE ? total : start + (last >> a.gshift) + 1;   // keys any row of the tile sees
+  const int k0 = split * a.chunk;
+  const int k1 = k0 + a.chunk < kend ? k0 + a.chunk : kend;
+  if (k0 >= k1) return;
+
+  if constexpr (TREE) {
+    // Ancestors of every node as bits, by doubling the step up the tree.  A parent that is not an
+    // earlier node of the sequence counts as none.
+    const int words = (n + 31) / 32;
+    for (int i = threadIdx.x; i < n; i += C::THREADS) {
+      const int p = a.parent[t0 + i];
+      up[i] = p >= 0 && p < i ? p : -1;
+      for (int w = 0; w < words; ++w) anc[i * MASK_WORDS + w] = w == i / 32 ? 1u << (i & 31) : 0u;
+    }
+    __syncthreads();
+    static_assert(C::THREADS >= MAX_NODES, "a thread per node");
+    for (int step = 1; step < n; step *= 2) {
+      const int i = threadIdx.x;
+      int p = -1;
+      uint32_t m[MASK_WORDS];
+      if (i < n && (p = up[i]) >= 0) {
+        for (int w = 0; w < words; ++w) m[w] = anc[p * MASK_WORDS + w];
+      }
+      const int pp = p >= 0 ? up[p] : -1;
+      __syncthreads();
+      if (p >= 0) {
+        for (int w = 0; w < words; ++w) anc[i * MASK_WORDS + w] |= m[w];
+        up[i] = pp;
+      }
+      __syncthreads();
+    }
+  }
+
+  // this lane's row
+  const int wrow = row0 + 32 * rw;
+  const int myrow = wrow + (lane & 31) < rows ? wrow + (lane & 31) : rows - 1;
+  const int r = myrow >> a.gshift, head = (g << a.gshift) + (myrow & (G - 1));
+  const bool active = wrow < rows;
+  const size_t qrow = (size_t)(t0 + r) * a.hq + head;
+  uint4 qf[T::KT];
+#pragma unroll
+  for (int t = 0; t < T::KT; ++t) qf[t] = ldg16((const char*)a.q + qrow * T::RB + (2 * t + h) * 16);
+  const int wfirst = (wrow < rows ? wrow : rows - 1) >> a.gshift;            // the wave's first token
+  const int wlast = (wrow + 31 < rows ? wrow + 31 : rows - 1) >> a.gshift;   // and its last
+  const int full = TREE ? start : start + wfirst + 1;   // keys below are seen by all its rows
+  const int some = TREE ? total : start + wlast + 1;    // keys from here on by none
+
+  // which keys of the block kb .. kb + 31 this lane's row sees
+  auto sees32 = [&](int kb) -> uint32_t {
+    if constexpr (TREE) {
+      const int d = kb - start;
+      if (d <= -32) return ~0u;
+      const uint32_t* m = anc + r * MASK_WORDS;
+      const int words = (n + 31) / 32;
+      if (d < 0) return m[0] << -d | ((1u << -d) - 1u);
+      const int w = d >> 5, s = d & 31;
+      const uint32_t lo = w < words ? m[w] : 0u, hi = w + 1 < words ? m[w + 1] : 0u;
+      return s ? lo >> s | hi << (32 - s) : lo;
+    } else {
+      const int nv = start + r + 1 - kb;
+      return nv >= 32 ? ~0u : nv <= 0 ? 0u : (1u << nv) - 1u;
+    }
+  };
+
+  // tile loads: 1024 bytes an instruction, the waves in turn
+  const char* kc = (const char*)a.k + (size_t)u * a.cap * T::RB;
+  const char* vc = (const char*)a.v + (size_t)u * a.cap * T::RB;
+  const uint32_t lds0 = lds_offset(lds);
+  auto load_tile = [&](int kb, int buf) {
+    constexpr int RPI = 1024 / T::RB;            // rows an instruction covers
+#pragma unroll
+    for (int x = 0; x < C::TILE / 1024 / C::NW; ++x) {
+      const int i = x * C::NW + wave;
+      const int row = i * RPI + lane / T::CH, p = lane % T::CH;
+      const int src = kb + row < total ? kb + row : total - 1;
+      load_to_lds16(kc + (size_t)src * T::RB + (p ^ T::kx(row)) * 16, lds0 + buf * C::BUF + i * 1024);
+      load_to_lds16(vc + (size_t)src * T::RB + (p ^ T::vx(row)) * 16,
+                    lds0 + buf * C::BUF + C::TILE + i * 1024);
+    }
+  };
+
+  const float c = a.scale * LOG2E;
+  f32x16_t o[D / 32];
+  float m, l;
+  const int ntile = (k1 - k0 + C::BN - 1) / C::BN;
+  // A second pass only if the first met a masked value row that is not finite (0 times it is NaN):
+  // its masked blocks go key by key.
+  for (int careful = 0; careful < 2; ++careful) {
+    m = NEG_INF;
+    l = 0.0f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) o[db] = f32x16_t{};
+    load_tile(k0, 0);
+    for (int it = 0; it < ntile; ++it) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      const int kt = k0 + it * C::BN;
+      if (it + 1 < ntile) load_tile(kt + C::BN, (it + 1) & 1);
+      const int kb = kt + kw * SK;
+      if (active && kb < k1 && kb < some) {
+        const char* kl = lds + (it & 1) * C::BUF + kw * SK * T::RB;
+        const char* vl = kl + C::TILE;
+        f32x16_t s[SK / 32];
+        float mx = NEG_INF;
+        const bool masked = kb + SK > full;
+#pragma unroll
+        for (int x = 0; x < SK / 32; ++x) {
+          s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
+          if (masked) {
+            const uint32_t w = sees32(kb + 32 * x) >> (4 * h);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[x][i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[x][i] : NEG_INF;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
+        }
+        const float mn = fmaxf(m, half_max(mx) * c);
+        if (__any(mn > m)) {
+          const float f = rescale(m, mn);
+          l *= f;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] *= f;
+          m = mn;
+        }
+        const float mc = m == NEG_INF ? 0.0f : m;
+#pragma unroll
+        for (int x = 0; x < SK / 32; ++x) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], c, -mc));
+            l += s[x][i];
+          }
+          if (careful && masked) values32_masked<DT, D>(vl + 32 * x * T::RB, s[x], sees32(kb + 32 * x), o, lane);
+          else values32<DT, D>(vl + 32 * x * T::RB, s[x], o, lane);
+        }
+      }
+    }
+    int bad = 0;
+    if (!careful) {
+      float z = 0.0f;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[db][i], 0.0f, z);
+      bad = active && !(z == 0.0f);
+    }
+    if (!__syncthreads_or(bad)) break;
+  }
+  l = half_sum(l);
+
+  // join the key groups: group 0 takes the others' results from LDS
+  if constexpr (KW > 1) {
+    if (kw > 0) {
+      char* p = lds + ((kw - 1) * RW + rw) * C::OB;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) reinterpret_cast<float*>(p)[(db * 16 + i) * 64 + lane] = o[db][i];
+      if (h == 0) {
+        reinterpret_cast<float*>(p + 32 * D * 4)[lane] = m;
+        reinterpret_cast<float*>(p + 32 * D * 4)[32 + lane] = l;
+      }
+    }
+    __syncthreads();
+    if (kw > 0) return;
+    float mm = m;
+#pragma unroll
+    for (int x = 1; x < KW; ++x)
+      mm = fmaxf(mm, reinterpret_cast<const float*>(lds + ((x - 1) * RW + rw) * C::OB + 32 * D * 4)[lane & 31]);
+    float f = rescale(m, mm);
+    l *= f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= f;
+#pragma unroll
+    for (int x = 1; x < KW; ++x) {
+      const char* p = lds + ((x - 1) * RW + rw) * C::OB;
+      const float* ml = reinterpret_cast<const float*>(p + 32 * D * 4);
+      const float mx = ml[lane & 31];
+      f = rescale(mx, mm);
+      l = __builtin_fmaf(ml[32 + (lane & 31)], f, l);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          o[db][i] = __builtin_fmaf(reinterpret_cast<const float*>(p)[(db * 16 + i) * 64 + lane], f, o[db][i]);
+    }
+    m = mm;
+  }
+  if (wrow + (lane & 31) >= rows) return;
+  if (a.splits > 1) {
+    float* po = a.part + (qrow * a.splits + split) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(po + 32 * db + 8 * q + 4 * h) =
+            make_float4(o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]);
+    if (h == 0)
+      *reinterpret_cast<float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D +
+                                 (qrow * a.splits + split) * 2) = make_float2(m, l);
+    return;
+  }
+  const float inv = 1.0f / l;
+  char* out = (char*)a.out + qrow * T::RB;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * db + 8 * q + 4 * h;
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = o[db][4 * q + e] * inv;
+      if constexpr (DT == 1)
+        *reinterpret_cast<uint2*>(out + d * 2) =
+            make_uint2(f32_to_bf16_bits(f[0]) | f32_to_bf16_bits(f[1]) << 16,
+                       f32_to_bf16_bits(f[2]) | f32_to_bf16_bits(f[3]) << 16);
+      else
+        *reinterpret_cast<float4*>(out + d * 4) = make_float4(f[0], f[1], f[2], f[3]);
+    }
+}
+
+// Joins the parts of the key range, a wave per row.
+template <int DT, int D>
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
+  constexpr int EPL = D / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int pairs = a.batch * a.hk;
+  const int pair = blockIdx.x % pairs, row = (blockIdx.x / pairs) * 4 + wave;
+  const int b = pair / a.hk, g = pair % a.hk;
+  const int u = (b * a.n_layers + a.layer) * a.hk + g;
+  int t0, n;
+  token_range(a.tok, b, t0, n);
+  if (row >= n << a.gshift) return;
+  const int r = row >> a.gshift, head = (g << a.gshift) + (row & ((1 << a.gshift) - 1));
+  const int keys = rows_before(a.unit_len, a.len, u) + (a.parent ? n : r + 1);
+  const int parts = (keys + a.chunk - 1) / a.chunk;       // those that a kernel wrote
+  const size_t qrow = (size_t)(t0 + r) * a.hq + head;
+  const float* po = a.part + qrow * a.splits * D;
+  const float* ml = a.part + (size_t)a.tok.tokens * a.hq * a.splits * D + qrow * a.splits * 2;
+  float m = NEG_INF;
+  for (int s = 0; s < parts; ++s) m = fmaxf(m, ml[2 * s]);
+  float l = 0.0f, o[EPL] = {};
+  for (int s = 0; s < parts; ++s) {
+    const float f = rescale(ml[2 * s], m);
+    l = __builtin_fmaf(ml[2 * s + 1], f, l);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(po[(size_t)s * D + lane * EPL + e], f, o[e]);
+  }
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
+    if constexpr (DT == 1)
+      reinterpret_cast<uint16_t*>(a.out)[qrow * D + lane * EPL + e] = (uint16_t)f32_to_bf16_bits(o[e] * inv);
+    else
+      reinterpret_cast<float*>(a.out)[qrow * D + lane * EPL + e] = o[e] * inv;
+  }
+}
+
+constexpr int CUS = 256;
+constexpr int FEW_ROWS = 32;         // rows of a sequence and KV head that one wave holds
+constexpr int MIN_CHUNK = 256;       // keys of a part, at least; a multiple of every key tile
+
+template <int DT, int D, int RW, int KW, int SK>
+int launch_cfg(const AttendArgs& a, hipStream_t s) {
+  using C = Cfg<DT, D, RW, KW, SK>;
+  const dim3 grid((unsigned)((int64_t)a.batch * a.hk * a.ntiles * a.splits));
+  if (a.parent) {
+    const auto k = attend_kernel<DT, D, RW, KW, SK, true>;
+    allow_lds((const void*)k, C::LDS);
+    hipLaunchKernelGGL(k, grid, dim3(C::THREADS), C::LDS, s, a);
+  } else {
+    const auto k = attend_kernel<DT, D, RW, KW, SK, false>;
+    allow_lds((const void*)k, C::LDS);
+    hipLaunchKernelGGL(k, grid, dim3(C::THREADS), C::LDS, s, a);
+  }
+  return (int)hipGetLastError();
+}
+
+// (float32 tiles of four key groups would not fit the LDS)
+bool few_rows(const AttendArgs& a, int dtype) {
+  return dtype == 1 && (int64_t)a.tok.max_tokens << a.gshift <= FEW_ROWS;
+}
+
+template <int DT, int D>
+int launch_type(const AttendArgs& a, hipStream_t s) {
+  int rc;
+  if constexpr (DT == 1)
+    rc = few_rows(a, DT) ? launch_cfg<DT, D, 1, 4, 32>(a, s) : launch_cfg<DT, D, 4, 1, 64>(a, s);
+  else
+    rc = launch_cfg<DT, D, 4, 1, 32>(a, s);
+  if (rc == 0 && a.splits > 1) {
+    const int64_t rows = (int64_t)a.tok.max_tokens << a.gshift;
+    hipLaunchKernelGGL((attend_join_kernel<DT, D>), dim3((unsigned)(a.batch * a.hk * ((rows + 3) / 4))),
+                       dim3(256), 0, s, a);
+    rc = (int)hipGetLastError();
+  }
+  return rc;
+}
+
+}  // namespace
+
+bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
+  const int64_t rows = (int64_t)a.tok.max_tokens << a.gshift;
+  const int bm = few_rows(a, dtype) ? 32 : 128;
+  const int64_t pairs = (int64_t)a.batch * a.hk;
+  const int64_t nt = (rows + bm - 1) / bm;
+  // row tiles in all: the packed tokens' and a part of one for every sequence
+  const int64_t all = ((int64_t)a.tok.tokens << a.gshift) * a.hk / bm + pairs;
+  const int64_t wgs = all < nt * pairs ? all : nt * pairs;
+  int64_t splits = 2 * CUS / wgs;
+  const int64_t most = (L + MIN_CHUNK - 1) / MIN_CHUNK;
+  splits = splits > most ? most : splits < 1 ? 1 : splits;
+  const int64_t chunk = ((L + splits - 1) / splits + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK;
+  a.splits = (int)splits;
+  a.chunk = (int)chunk;
+  a.ntiles = (int)nt;
+  return pairs * nt * splits < (1ll << 31) && pairs * ((rows + 3) / 4) < (1ll << 31);
+}
+
+int launch_attend(const AttendArgs& a, int dtype, int D, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == 1) return D == 128 ? launch_type<1, 128>(a, s) : launch_type<1, 64>(a, s);
+  return D == 128 ? launch_type<0, 128>(a, s) : launch_type<0, 64>(a, s);
+}
+
+}  // namespace dc

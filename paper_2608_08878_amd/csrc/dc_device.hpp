@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "dc_kernels.hpp"
+
 namespace dc {
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -150,6 +152,38 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 ldg16_nt(const void* p) {
   const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
   return make_uint4(v.x, v.y, v.z, v.w);
+}
+
+// The packed tokens t0 .. t0 + n - 1 of sequence b.  Offsets that are no ascending
+// partition of the tokens are clamped, so that no index leaves the arrays.
+__device__ __forceinline__ void token_range(const TokenArgs& t, int b, int& t0, int& n) {
+  if (!t.cu) {
+    t0 = b * t.max_tokens;
+    n = t.max_tokens;
+    return;
+  }
+  const int c0 = t.cu[b], c1 = t.cu[b + 1];
+  t0 = c0 < 0 ? 0 : c0 > t.tokens ? t.tokens : c0;
+  const int t1 = c1 < t0 ? t0 : c1 > t.tokens ? t.tokens : c1;
+  n = t1 - t0 < t.max_tokens ? t1 - t0 : t.max_tokens;
+}
+
+// Rows of unit u before a call's own (len: their bound).
+__device__ __forceinline__ int rows_before(const int32_t* unit_len, int len, int u) {
+  if (!unit_len) return len;
+  const int x = unit_len[u];
+  return x < 0 ? 0 : x > len ? len : x;
+}
+
+__device__ __forceinline__ void compiler_fence() { asm volatile("" ::: "memory"); }
+
+// 16 bytes per lane from global memory to LDS byte lds + 16 lane (lds uniform).
+// Issued from inline assembly, out of the compiler's sight: the caller waits
+// for it explicitly (vmcnt; loads complete in issue order).  A load into LDS
+// needs one wait state after a scalar write of M0 (the s_nop).
+__device__ __forceinline__ void load_to_lds16(const void* g, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               : : "v"(g), "s"(lds) : "memory", "m0");
 }
 
 }  // namespace dc

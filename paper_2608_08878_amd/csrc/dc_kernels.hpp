@@ -144,6 +144,73 @@ struct GlobalAlphaArgs {
   int y0;                   // first grid row of the launch (see for_grid_y)
 };
 
+// The packed tokens of one call as a kernel sees them.
+struct TokenArgs {
+  const int32_t* cu;        // [batch + 1] first token of every sequence, or null: max_tokens each
+  int tokens;               // N, all sequences'
+  int max_tokens;           // bound of one sequence's
+};
+
+// Norm and rotation of the packed tokens' query and key heads (dc_rows.hip).
+struct NormRopeArgs {
+  const void* q;            // [N][hq][D], ld_q elements from token to token
+  const void* k;            // [N][hk][D]
+  const void* v;            // [N][hk][D] (cache form only)
+  int64_t ld_q, ld_k, ld_v;
+  const int32_t* pos;       // [N]
+  const float* q_gain;      // [D] or null (ones)
+  const float* k_gain;
+  const float* inv_freq;    // [rot / 2]
+  void* q_out;              // [N][hq][D]
+  void* k_out;              // [N][hk][D], or null: the rows go to the cache
+  void* kc;                 // [units][cap][D]
+  void* vc;
+  const int32_t* unit_len;  // [units] or null: len each
+  int64_t cap;
+  TokenArgs tok;
+  int batch, n_layers, layer, hq, hk, len;
+  int norm, rot, interleaved;
+  float eps;
+};
+
+// Attention of the packed tokens over cache rows (dc_attend.hip).
+struct AttendArgs {
+  const void* q;            // [N][hq][D]
+  void* out;                // [N][hq][D]
+  const void* k;            // [units][cap][D]
+  const void* v;
+  const int32_t* unit_len;  // [units] rows before the tokens' own, or null: len each
+  const int32_t* parent;    // [N] parents of drafted tokens, or null: causal
+  float* part;              // [N hq][splits][D] outputs, then [N hq][splits][2] (m, l); null if splits = 1
+  int64_t cap;
+  TokenArgs tok;
+  int batch, n_layers, layer, hq, hk, gshift, len;
+  float scale;
+  int splits;               // parts of the key range, `chunk` rows each
+  int chunk;
+  int ntiles;               // row tiles of the longest sequence
+};
+
+// The rows behind each unit's length become part of the cache (dc_rows.hip).
+struct CommitArgs {
+  void* k;
+  void* v;
+  float* alpha;             // feature state, or null
+  double* num;
+  double* den;
+  int32_t* pos;
+  float* vnorm;
+  float* sigma;
+  int32_t* unit_len;        // [units] or null
+  const int32_t* path;      // [batch][width] or null
+  const int32_t* keep;      // [batch] or null
+  int64_t cap;
+  TokenArgs tok;
+  int units, per_seq;       // per_seq = units of one sequence
+  int len, width, next_pos;
+  int y0;                   // first grid row of the launch (see for_grid_y)
+};
+
 // Grids whose rows are units (or unit groups) are launched in slices of at
 // most MAX_GRID_Y rows (the hardware limit of a grid's y dimension): f(y0, ny)
 // launches rows y0 .. y0 + ny - 1, the kernel adding y0 to blockIdx.y.
@@ -195,5 +262,11 @@ bool step_fits(int L, int G, int D, bool feat, int nmoves);
 int step_ragged_rows(int G, int D);
 int step_chunk_rows();
 int kl_tile_cols();
+int launch_norm_rope(const NormRopeArgs& a, int dtype, int D, void* stream);
+int launch_commit(const CommitArgs& a, int dtype, int D, void* stream);
+// How a call of these sizes is cut (a.splits, a.chunk, a.ntiles), for caches of up to L
+// rows, the tokens' own included; returns false when its grid is out of range.
+bool attend_plan(AttendArgs& a, int dtype, int D, int L);
+int launch_attend(const AttendArgs& a, int dtype, int D, void* stream);
 
 }  // namespace dc

@@ -37,17 +37,7 @@ constexpr int KL_NS = 5;                 // stage buffers (50 KB: two workgroups
 
 typedef __attribute__((address_space(3))) char lds_char_t;
 
-__device__ __forceinline__ void compiler_fence() { asm volatile("" ::: "memory"); }
-
-// 16 bytes per lane from global memory to LDS byte lds + 16 lane (lds uniform).
-// Issued from inline assembly, out of the compiler's sight: the caller waits
-// for it explicitly (vmcnt; loads complete in issue order).  A load into LDS
-// needs one wait state after a scalar write of M0 (the s_nop).
-__device__ __forceinline__ void load_to_lds16(const void* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-               : : "v"(g), "s"(lds) : "memory", "m0");
-}
-// The same with the non-temporal hint: for data read once per call (the
+// load_to_lds16 with the non-temporal hint: for data read once per call (the
 // per-step kernel's lm head), which then does not displace cached lines --
 // dirty lines of earlier kernels among them, whose write-back would otherwise
 // share the HBM with the stream.

@@ -1,0 +1,271 @@
+// Rows of several tokens on their way into a cache, on gfx950: the norm of query and
+// key heads with the rotation by position, and the commit of rows behind the cache's
+// length (a prompt's, or the accepted path of a draft tree).  Both move bytes.
+#include "dc_device.hpp"
+#include "dc_kernels.hpp"
+
+#pragma clang fp contract(off)
+
+namespace dc {
+
+namespace {
+
+constexpr int RT = 256;               // threads of a workgroup
+constexpr int MAX_PAIRS = 64;         // rotated pairs of a head of 128
+constexpr double INV_2PI = 0.15915494309189533577;
+
+template <int DTYPE>
+__device__ __forceinline__ uint4 pack_slice(const float* f) {
+  if constexpr (DTYPE == 1)
+    return make_uint4(f32_to_bf16_bits(f[0]) | f32_to_bf16_bits(f[1]) << 16,
+                      f32_to_bf16_bits(f[2]) | f32_to_bf16_bits(f[3]) << 16,
+                      f32_to_bf16_bits(f[4]) | f32_to_bf16_bits(f[5]) << 16,
+                      f32_to_bf16_bits(f[6]) | f32_to_bf16_bits(f[7]) << 16);
+  else
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+}
+
+// y = x / sqrt(mean x^2 + eps) * gain, then pairs (a, b) of the first rot elements turn
+// by phi = pos f_i: (a cos phi - b sin phi, a sin phi + b cos phi), pair i being
+// elements (i, i + rot / 2), or (2 i, 2 i + 1) interleaved.  float32 between the load
+// and the one rounding at the store.  A far position times a frequency is a million
+// radians and more, of which float32 keeps no useful fraction of a turn: the product is
+// formed in binary64 (exact: 31 + 24 bits, one rounding) and taken to turns there; the
+// remaining fraction goes to float32 sinpi / cospi.
+// A workgroup takes one token at a time: its angles once in LDS for every head, then
+// LPR lanes per head row, 16 bytes each, the half-split partner a lane exchange away.
+template <int DTYPE, int D>
+__global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_block) {
+  using R = RowT<DTYPE, D>;
+  constexpr int LPR = R::LPR, EPL = R::EPL, ELT = R::ELT, GROUPS = RT / LPR;
+  __shared__ float cs[MAX_PAIRS], sn[MAX_PAIRS];
+  const int tid = threadIdx.x, c = tid % LPR, grp = tid / LPR;
+  const int half = a.rot / 2, dist = half / EPL;      // half-split partner: dist lanes away
+  const int nrows = a.hq + a.hk + (a.k_out ? 0 : a.hk);
+  const int first = blockIdx.x * per_block;
+  for (int t = first; t < first + per_block && t < a.tok.tokens; ++t) {
+    if (tid < half) {
+      const double turns = (double)a.pos[t] * (double)a.inv_freq[tid] * INV_2PI;
+      const float f = (float)(2.0 * (turns - rint(turns)));
+      sincospif(f, &sn[tid], &cs[tid]);
+    }
+    // the sequence of token t and its number there (cache form)
+    int b = 0, r = 0;
+    bool owned = true;
+    if (!a.k_out) {
+      if (a.tok.cu) {
+        int lo = 0, hi = a.batch;             // the last b with cu[b] <= t
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (a.tok.cu[mid] <= t) lo = mid; else hi = mid;
+        }
+        b = lo;
+      } else {
+        b = t / a.tok.max_tokens;
+      }
+      int t0, n;
+      token_range(a.tok, b, t0, n);
+      r = t - t0;
+      owned = r >= 0 && r < n;
+    }
+    __syncthreads();
+    for (int row = grp; row < nrows; row += GROUPS) {
+      const bool isq = row < a.hq, isv = row >= a.hq + a.hk;
+      const int h = isq ? row : isv ? row - a.hq - a.hk : row - a.hq;
+      const char* src = (const char*)(isq ? a.q : isv ? a.v : a.k) +
+                        ((size_t)t * (isq ? a.ld_q : isv ? a.ld_v : a.ld_k) + (size_t)h * D) * ELT;
+      uint4 w = ldg16(src + c * 16);
+      if (!isv) {
+        float x[EPL];
+        unpack_slice<DTYPE>(w, x);
+        if (a.norm) {
+          float s = x[0] * x[0];
+#pragma unroll
+          for (int e = 1; e < EPL; ++e) s = __builtin_fmaf(x[e], x[e], s);
+          s = row_sum<LPR>(s);
+          const float inv = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
+          const float* gain = isq ? a.q_gain : a.k_gain;
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * (gain ? gain[c * EPL + e] : 1.0f);
+        }
+        if (a.interleaved) {
+          if (c * EPL < a.rot) {
+#pragma unroll
+            for (int e = 0; e < EPL; e += 2) {
+              const float co = cs[(c * EPL + e) / 2], si = sn[(c * EPL + e) / 2];
+              const float p = x[e], o = x[e + 1];
+              x[e] = __builtin_fmaf(p, co, -(o * si));
+              x[e + 1] = __builtin_fmaf(p, si, o * co);
+            }
+          }
+        } else if (half) {
+          const bool low = c < dist, in = c < 2 * dist;
+          const int from = in ? (low ? c + dist : c - dist) : c;
+          const int i0 = in ? (low ? c : c - dist) * EPL : 0;
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) {
+            const float o = __shfl(x[e], from, LPR);
+            const float co = cs[i0 + e], si = low ? -sn[i0 + e] : sn[i0 + e];
+            if (in) x[e] = __builtin_fmaf(x[e], co, o * si);
+          }
+        }
+        w = pack_slice<DTYPE>(x);
+      }
+      char* dst;
+      if (isq) {
+        dst = (char*)a.q_out + ((size_t)t * a.hq + h) * D * ELT;
+      } else if (a.k_out) {
+        dst = (char*)a.k_out + ((size_t)t * a.hk + h) * D * ELT;
+      } else {
+        const int u = (b * a.n_layers + a.layer) * a.hk + h;
+        dst = (char*)(isv ? a.vc : a.kc) +
+              ((size_t)u * a.cap + rows_before(a.unit_len, a.len, u) + r) * D * ELT;
+      }
+      if (isq || owned) *reinterpret_cast<uint4*>(dst + c * 16) = w;
+    }
+    __syncthreads();
+  }
+}
+
+// Rows that unit u keeps of its n new ones.
+__device__ __forceinline__ int rows_kept(const CommitArgs& a, int b, int n) {
+  int m = n < a.width ? n : a.width;
+  if (a.keep) {
+    const int x = a.keep[b];
+    m = x < 0 ? 0 : x < m ? x : m;
+  }
+  return m;
+}
+
+// Feature state of a row as dc_feat_init leaves it (lane c of the row's LPR).
+template <int DTYPE, int D>
+__device__ __forceinline__ void init_row(const CommitArgs& a, int u, int slot, int j, const uint4& v,
+                                         int c) {
+  using R = RowT<DTYPE, D>;
+  float f[R::EPL];
+  unpack_slice<DTYPE>(v, f);
+  float s = f[0] * f[0];
+#pragma unroll
+  for (int e = 1; e < R::EPL; ++e) s = __builtin_fmaf(f[e], f[e], s);
+  s = row_sum<R::LPR>(s);
+  if (c == 0) {
+    const size_t i = (size_t)u * a.cap + slot;
+    a.alpha[i] = 0.0f;
+    a.num[i] = 0.0;
+    a.den[i] = 0.0;
+    a.pos[i] = a.next_pos + j;
+    a.vnorm[i] = sqrtf(s);
+    if (a.sigma) a.sigma[i] = 0.0f;
+  }
+}
+
+// An accepted path: row len + j <- row len + path[j].  One workgroup per unit walks the
+// path in passes of RT / LPR rows; a pass has read its rows before it writes, and an
+// entry below its own index counts as that index, so no later pass reads a row that an
+// earlier one has written.
+template <int DTYPE, int D>
+__global__ void __launch_bounds__(RT) commit_path_kernel(CommitArgs a) {
+  using R = RowT<DTYPE, D>;
+  constexpr int LPR = R::LPR, RPP = RT / LPR;
+  const int u = a.y0 + blockIdx.x, b = u / a.per_seq;
+  const int c = threadIdx.x % LPR, jr = threadIdx.x / LPR;
+  int t0, n;
+  token_range(a.tok, b, t0, n);
+  const int start = rows_before(a.unit_len, a.len, u), keep = rows_kept(a, b, n);
+  for (int j0 = 0; j0 < keep; j0 += RPP) {
+    const int j = j0 + jr;
+    const bool on = j < keep;
+    int src = on ? a.path[(size_t)b * a.width + j] : 0;
+    src = src < j ? j : src >= n ? n - 1 : src;
+    const size_t from = (((size_t)u * a.cap + start + src) * LPR + c) * 16;
+    const size_t to = (((size_t)u * a.cap + start + j) * LPR + c) * 16;
+    uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
+    if (on) {
+      kw = ldg16((const char*)a.k + from);
+      vw = ldg16((const char*)a.v + from);
+    }
+    __syncthreads();
+    if (on) {
+      *reinterpret_cast<uint4*>((char*)a.k + to) = kw;
+      *reinterpret_cast<uint4*>((char*)a.v + to) = vw;
+    }
+    if (a.alpha && on) init_row<DTYPE, D>(a, u, start + j, j, vw, c);
+  }
+  if (a.unit_len) {
+    __syncthreads();
+    if (threadIdx.x == 0) a.unit_len[u] = start + keep;
+  }
+}
+
+// The first rows as they are: only their feature state is written.
+template <int DTYPE, int D>
+__global__ void __launch_bounds__(RT) commit_rows_kernel(CommitArgs a) {
+  using R = RowT<DTYPE, D>;
+  constexpr int LPR = R::LPR, RPP = RT / LPR;
+  const int u = a.y0 + blockIdx.y, b = u / a.per_seq;
+  const int c = threadIdx.x % LPR;
+  int t0, n;
+  token_range(a.tok, b, t0, n);
+  const int start = rows_before(a.unit_len, a.len, u), keep = rows_kept(a, b, n);
+  for (int j = blockIdx.x * RPP + threadIdx.x / LPR; j < keep; j += gridDim.x * RPP)
+    init_row<DTYPE, D>(a, u, start + j, j,
+                       ldg16((const char*)a.v + (((size_t)u * a.cap + start + j) * LPR + c) * 16), c);
+}
+
+__global__ void commit_len_kernel(CommitArgs a) {
+  const int u = blockIdx.x * RT + threadIdx.x;
+  if (u >= a.units) return;
+  const int b = u / a.per_seq;
+  int t0, n;
+  token_range(a.tok, b, t0, n);
+  a.unit_len[u] = rows_before(a.unit_len, a.len, u) + rows_kept(a, b, n);
+}
+
+template <int DTYPE, int D>
+void norm_rope(const NormRopeArgs& a, hipStream_t s) {
+  const int per = a.tok.tokens >= 8192 ? 4 : 1;
+  hipLaunchKernelGGL((norm_rope_kernel<DTYPE, D>), dim3((a.tok.tokens + per - 1) / per), dim3(RT), 0, s, a,
+                     per);
+}
+
+template <int DTYPE, int D>
+void commit(const CommitArgs& a, hipStream_t s) {
+  if (a.path) {
+    hipLaunchKernelGGL((commit_path_kernel<DTYPE, D>), dim3(a.units), dim3(RT), 0, s, a);
+    return;
+  }
+  if (a.alpha) {
+    constexpr int RPP = RT / RowT<DTYPE, D>::LPR;
+    const int gx = (a.width + RPP - 1) / RPP < 64 ? (a.width + RPP - 1) / RPP : 64;
+    for_grid_y(a.units, [&](int y0, int ny) {
+      CommitArgs b = a;
+      b.y0 = y0;
+      hipLaunchKernelGGL((commit_rows_kernel<DTYPE, D>), dim3(gx, ny), dim3(RT), 0, s, b);
+    });
+  }
+  if (a.unit_len) hipLaunchKernelGGL(commit_len_kernel, dim3((a.units + RT - 1) / RT), dim3(RT), 0, s, a);
+}
+
+}  // namespace
+
+int launch_norm_rope(const NormRopeArgs& a, int dtype, int D, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == 1 && D == 128) norm_rope<1, 128>(a, s);
+  else if (dtype == 1) norm_rope<1, 64>(a, s);
+  else if (D == 128) norm_rope<0, 128>(a, s);
+  else norm_rope<0, 64>(a, s);
+  return (int)hipGetLastError();
+}
+
+int launch_commit(const CommitArgs& a, int dtype, int D, void* stream) {
+  if (!a.path && !a.alpha && !a.unit_len) return 0;      // the host's lengths say it all
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == 1 && D == 128) commit<1, 128>(a, s);
+  else if (dtype == 1) commit<1, 64>(a, s);
+  else if (D == 128) commit<0, 128>(a, s);
+  else commit<0, 64>(a, s);
+  return (int)hipGetLastError();
+}
+
+}  // namespace dc
