@@ -14,6 +14,8 @@
 // order of the sum being free as long as V is read in the same one.  K and V tiles go from memory
 // to LDS directly (their 16-byte chunks permuted at the source so that operand reads spread over the
 // banks); bf16 V is read through the transposing LDS load.
+#include <type_traits>
+
 #include "dc_device.hpp"
 #include "dc_kernels.hpp"
 #include "distillcache.h"
@@ -70,6 +72,11 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 __device__ __forceinline__ float rescale(float m, float mn) {
   return m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
 }
+
+// A row keeps its maximum while no key exceeds it by more than this (in powers of two): weights are
+// then at most 2^SLACK instead of 1, which float32 sums and bf16 weights hold as well, and the
+// accumulators are rescaled once or twice in a long row instead of at every new maximum.
+constexpr float SLACK = 8.0f;
 
 // Key held by accumulator register i of a lane in half h of the wave: bit i of a 32-key block.
 __device__ __forceinline__ int key_of(int i, int h) { return 8 * (i / 4) + 4 * h + i % 4; }
@@ -182,7 +189,7 @@ struct Cfg {
 };
 
 template <int DT, int D, int RW, int KW, int SK, bool TREE>
-__global__ void __launch_bounds__(64 * RW * KW) attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) attend_kernel(AttendArgs a) {
   using T = KVT<DT, D>;
   using C = Cfg<DT, D, RW, KW, SK>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -292,70 +299,76 @@ __global__ void __launch_bounds__(64 * RW * KW) attend_kernel(AttendArgs a) {
   f32x16_t o[D / 32];
   float m, l;
   const int ntile = (k1 - k0 + C::BN - 1) / C::BN;
-  // A second pass only if the first met a masked value row that is not finite (0 times it is NaN):
-  // its masked blocks go key by key.
-  for (int careful = 0; careful < 2; ++careful) {
+  // One pass over the keys.  CAREFUL: masked blocks go key by key.
+  auto pass = [&](auto careful) {
+    constexpr bool CAREFUL = decltype(careful)::value;
     m = NEG_INF;
     l = 0.0f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16_t{};
-    load_tile(k0, 0);
-    for (int it = 0; it < ntile; ++it) {
+    // a tile in buffer BUF; the next one's loads are under way meanwhile
+    auto tile_step = [&](int it, auto bufc) {
+      constexpr int BUF = decltype(bufc)::value;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       const int kt = k0 + it * C::BN;
-      if (it + 1 < ntile) load_tile(kt + C::BN, (it + 1) & 1);
+      if (it + 1 < ntile) load_tile(kt + C::BN, 1 - BUF);
       const int kb = kt + kw * SK;
-      if (active && kb < k1 && kb < some) {
-        const char* kl = lds + (it & 1) * C::BUF + kw * SK * T::RB;
-        const char* vl = kl + C::TILE;
-        f32x16_t s[SK / 32];
-        float mx = NEG_INF;
-        const bool masked = kb + SK > full;
+      if (!active || kb >= k1 || kb >= some) return;
+      const char* kl = lds + BUF * C::BUF + kw * SK * T::RB;
+      const char* vl = kl + C::TILE;
+      f32x16_t s[SK / 32];
+      float mx = NEG_INF;
+      const bool masked = kb + SK > full;
 #pragma unroll
-        for (int x = 0; x < SK / 32; ++x) {
-          s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
-          if (masked) {
-            const uint32_t w = sees32(kb + 32 * x) >> (4 * h);
+      for (int x = 0; x < SK / 32; ++x) {
+        s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
+        if (masked) {
+          const uint32_t w = sees32(kb + 32 * x) >> (4 * h);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[x][i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[x][i] : NEG_INF;
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
+          for (int i = 0; i < 16; ++i) s[x][i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[x][i] : NEG_INF;
         }
-        const float mn = fmaxf(m, half_max(mx) * c);
-        if (__any(mn > m)) {
-          const float f = rescale(m, mn);
-          l *= f;
 #pragma unroll
-          for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[db][i] *= f;
-          m = mn;
-        }
-        const float mc = m == NEG_INF ? 0.0f : m;
-#pragma unroll
-        for (int x = 0; x < SK / 32; ++x) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            s[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], c, -mc));
-            l += s[x][i];
-          }
-          if (careful && masked) values32_masked<DT, D>(vl + 32 * x * T::RB, s[x], sees32(kb + 32 * x), o, lane);
-          else values32<DT, D>(vl + 32 * x * T::RB, s[x], o, lane);
-        }
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
       }
-    }
-    int bad = 0;
-    if (!careful) {
-      float z = 0.0f;
+      const float mn = fmaxf(m, half_max(mx) * c);
+      if (__any(mn > m + SLACK)) {
+        const float f = rescale(m, mn);
+        l *= f;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[db][i], 0.0f, z);
-      bad = active && !(z == 0.0f);
+          for (int i = 0; i < 16; ++i) o[db][i] *= f;
+        m = mn;
+      }
+      const float mc = m == NEG_INF ? 0.0f : m;
+#pragma unroll
+      for (int x = 0; x < SK / 32; ++x) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], c, -mc));
+          l += s[x][i];
+        }
+        if (CAREFUL && masked) values32_masked<DT, D>(vl + 32 * x * T::RB, s[x], sees32(kb + 32 * x), o, lane);
+        else values32<DT, D>(vl + 32 * x * T::RB, s[x], o, lane);
+      }
+    };
+    load_tile(k0, 0);
+    for (int it = 0; it < ntile; it += 2) {
+      tile_step(it, std::integral_constant<int, 0>{});
+      if (it + 1 < ntile) tile_step(it + 1, std::integral_constant<int, 1>{});
     }
-    if (!__syncthreads_or(bad)) break;
+  };
+  pass(std::false_type{});
+  // Again, carefully, only if a masked value row was met that is not finite (0 times it is NaN).
+  float z = 0.0f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[db][i], 0.0f, z);
+  if (__syncthreads_or(active && !(z == 0.0f))) {
+    pass(std::true_type{});
+    __syncthreads();
   }
   l = half_sum(l);
 
