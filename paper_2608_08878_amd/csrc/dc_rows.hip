@@ -14,13 +14,16 @@ constexpr int RT = 256;               // threads of a workgroup
 constexpr int MAX_PAIRS = 64;         // rotated pairs of a head of 128
 constexpr double INV_2PI = 0.15915494309189533577;
 
+// Two float32 numbers rounded to bf16 (to nearest even, NaN kept) in one instruction.
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
+}
+
 template <int DTYPE>
 __device__ __forceinline__ uint4 pack_slice(const float* f) {
   if constexpr (DTYPE == 1)
-    return make_uint4(f32_to_bf16_bits(f[0]) | f32_to_bf16_bits(f[1]) << 16,
-                      f32_to_bf16_bits(f[2]) | f32_to_bf16_bits(f[3]) << 16,
-                      f32_to_bf16_bits(f[4]) | f32_to_bf16_bits(f[5]) << 16,
-                      f32_to_bf16_bits(f[6]) | f32_to_bf16_bits(f[7]) << 16);
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
   else
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
                       __float_as_uint(f[3]));
@@ -31,100 +34,145 @@ __device__ __forceinline__ uint4 pack_slice(const float* f) {
 // elements (i, i + rot / 2), or (2 i, 2 i + 1) interleaved.  float32 between the load
 // and the one rounding at the store.  A far position times a frequency is a million
 // radians and more, of which float32 keeps no useful fraction of a turn: the product is
-// formed in binary64 (exact: 31 + 24 bits, one rounding) and taken to turns there; the
+// formed in binary64 (31 + 24 bits, one rounding) and taken to turns there; the
 // remaining fraction goes to float32 sinpi / cospi.
-// A workgroup takes one token at a time: its angles once in LDS for every head, then
-// LPR lanes per head row, 16 bytes each, the half-split partner a lane exchange away.
-template <int DTYPE, int D>
-__global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_block) {
+// A workgroup takes up to TPB tokens.  It first puts their angles and places in LDS, one
+// angle per thread, for every head; then LPR lanes work on a head row, 16 bytes each, the
+// half-split partner a lane exchange away, with BATCH rows' loads under way at a time.
+// One token and one row per lane group where that makes no more than FEW_WGS workgroups (a step's
+// 16 tokens 8.4 -> 6.3 us, 1557 float32 tokens 6.4 -> 5.3), else TPB tokens: a workgroup's angles and
+// places cost about 2 us of latency before its first store (16k tokens 437 us one at a time).
+// 20001 tokens of 32 + 16 heads of 128, 481 MB: 127 us = 3.8 TB/s, of the 4.8 that a copy reaches;
+// plain loads 138, three rows in flight 138 (fewer waves fit), tokens by two 157.
+constexpr int TPB = 4;
+constexpr int FEW_WGS = 4096;
+
+template <int DTYPE, int D, int BATCH>
+__global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_block, int passes) {
   using R = RowT<DTYPE, D>;
   constexpr int LPR = R::LPR, EPL = R::EPL, ELT = R::ELT, GROUPS = RT / LPR;
-  __shared__ float cs[MAX_PAIRS], sn[MAX_PAIRS];
+  __shared__ __attribute__((aligned(16))) float cs[TPB][MAX_PAIRS], sn[TPB][MAX_PAIRS];
+  __shared__ int seq[TPB], num[TPB];                  // a token's sequence and number there, or -1
   const int tid = threadIdx.x, c = tid % LPR, grp = tid / LPR;
   const int half = a.rot / 2, dist = half / EPL;      // half-split partner: dist lanes away
   const int nrows = a.hq + a.hk + (a.k_out ? 0 : a.hk);
   const int first = blockIdx.x * per_block;
-  for (int t = first; t < first + per_block && t < a.tok.tokens; ++t) {
-    if (tid < half) {
-      const double turns = (double)a.pos[t] * (double)a.inv_freq[tid] * INV_2PI;
-      const float f = (float)(2.0 * (turns - rint(turns)));
-      sincospif(f, &sn[tid], &cs[tid]);
-    }
-    // the sequence of token t and its number there (cache form)
-    int b = 0, r = 0;
-    bool owned = true;
-    if (!a.k_out) {
-      if (a.tok.cu) {
-        int lo = 0, hi = a.batch;             // the last b with cu[b] <= t
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) / 2;
-          if (a.tok.cu[mid] <= t) lo = mid; else hi = mid;
-        }
-        b = lo;
-      } else {
-        b = t / a.tok.max_tokens;
+  const int count = a.tok.tokens - first < per_block ? a.tok.tokens - first : per_block;
+  // this workgroup's rows of every token: GROUPS a pass
+  const int row0 = blockIdx.y * passes * GROUPS;
+  const int items = count * passes;
+
+  uint4 w[BATCH];
+  auto load = [&](int i) -> uint4 {
+    const int t = i / passes, row = row0 + (i - t * passes) * GROUPS + grp;
+    if (i >= items || row >= nrows) return make_uint4(0, 0, 0, 0);
+    const bool isq = row < a.hq, isv = row >= a.hq + a.hk;
+    const int h = isq ? row : isv ? row - a.hq - a.hk : row - a.hq;
+    const char* base = (const char*)(isq ? a.q : isv ? a.v : a.k);
+    const int64_t ld = isq ? a.ld_q : isv ? a.ld_v : a.ld_k;
+    return ldg16_nt(base + ((size_t)(first + t) * ld + (size_t)h * D) * ELT + c * 16);
+  };
+#pragma unroll
+  for (int x = 0; x < BATCH; ++x) w[x] = load(x);
+
+  for (int i = tid; i < count * half; i += RT) {
+    const int t = i / half, p = i - t * half;
+    const double turns = (double)a.pos[first + t] * (double)a.inv_freq[p] * INV_2PI;
+    sincospif((float)(2.0 * (turns - rint(turns))), &sn[t][p], &cs[t][p]);
+  }
+  if (!a.k_out && tid < count) {
+    const int t = first + tid;
+    int b = 0, r;
+    if (a.tok.cu) {
+      int lo = 0, hi = a.batch;             // the last b with cu[b] <= t
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.tok.cu[mid] <= t) lo = mid; else hi = mid;
       }
-      int t0, n;
-      token_range(a.tok, b, t0, n);
-      r = t - t0;
-      owned = r >= 0 && r < n;
+      b = lo;
+    } else {
+      b = t / a.tok.max_tokens;
     }
-    __syncthreads();
-    for (int row = grp; row < nrows; row += GROUPS) {
-      const bool isq = row < a.hq, isv = row >= a.hq + a.hk;
-      const int h = isq ? row : isv ? row - a.hq - a.hk : row - a.hq;
-      const char* src = (const char*)(isq ? a.q : isv ? a.v : a.k) +
-                        ((size_t)t * (isq ? a.ld_q : isv ? a.ld_v : a.ld_k) + (size_t)h * D) * ELT;
-      uint4 w = ldg16(src + c * 16);
-      if (!isv) {
-        float x[EPL];
-        unpack_slice<DTYPE>(w, x);
-        if (a.norm) {
-          float s = x[0] * x[0];
+    int t0, n;
+    token_range(a.tok, b, t0, n);
+    r = t - t0;
+    seq[tid] = b;
+    num[tid] = r >= 0 && r < n ? r : -1;
+  }
+  float gq[EPL], gk[EPL];
 #pragma unroll
-          for (int e = 1; e < EPL; ++e) s = __builtin_fmaf(x[e], x[e], s);
-          s = row_sum<LPR>(s);
-          const float inv = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
-          const float* gain = isq ? a.q_gain : a.k_gain;
+  for (int e = 0; e < EPL; ++e) {
+    gq[e] = a.q_gain ? a.q_gain[c * EPL + e] : 1.0f;
+    gk[e] = a.k_gain ? a.k_gain[c * EPL + e] : 1.0f;
+  }
+  __syncthreads();
+
+  auto finish = [&](int i, uint4 x16) {
+    const int t = i / passes, row = row0 + (i - t * passes) * GROUPS + grp;
+    if (i >= items || row >= nrows) return;
+    const bool isq = row < a.hq, isv = row >= a.hq + a.hk;
+    const int h = isq ? row : isv ? row - a.hq - a.hk : row - a.hq;
+    if (!isv) {
+      float x[EPL];
+      unpack_slice<DTYPE>(x16, x);
+      if (a.norm) {
+        float s = x[0] * x[0];
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * (gain ? gain[c * EPL + e] : 1.0f);
-        }
-        if (a.interleaved) {
-          if (c * EPL < a.rot) {
+        for (int e = 1; e < EPL; ++e) s = __builtin_fmaf(x[e], x[e], s);
+        s = row_sum<LPR>(s);
+        const float inv = rsqrtf(s * (1.0f / D) + a.eps);
 #pragma unroll
-            for (int e = 0; e < EPL; e += 2) {
-              const float co = cs[(c * EPL + e) / 2], si = sn[(c * EPL + e) / 2];
-              const float p = x[e], o = x[e + 1];
-              x[e] = __builtin_fmaf(p, co, -(o * si));
-              x[e + 1] = __builtin_fmaf(p, si, o * co);
-            }
+        for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * (isq ? gq[e] : gk[e]);
+      }
+      if (a.interleaved) {
+        if (c * EPL < a.rot) {
+#pragma unroll
+          for (int e = 0; e < EPL; e += 2) {
+            const float co = cs[t][(c * EPL + e) / 2], si = sn[t][(c * EPL + e) / 2];
+            const float p = x[e], o = x[e + 1];
+            x[e] = __builtin_fmaf(p, co, -(o * si));
+            x[e + 1] = __builtin_fmaf(p, si, o * co);
           }
-        } else if (half) {
-          const bool low = c < dist, in = c < 2 * dist;
-          const int from = in ? (low ? c + dist : c - dist) : c;
-          const int i0 = in ? (low ? c : c - dist) * EPL : 0;
+        }
+      } else if (half) {
+        const bool low = c < dist, in = c < 2 * dist;
+        const int from = in ? (low ? c + dist : c - dist) : c;
+        const int i0 = in ? (low ? c : c - dist) * EPL : 0;
+        float o[EPL];
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) o[e] = __shfl(x[e], from, LPR);
+        if (in) {
 #pragma unroll
           for (int e = 0; e < EPL; ++e) {
-            const float o = __shfl(x[e], from, LPR);
-            const float co = cs[i0 + e], si = low ? -sn[i0 + e] : sn[i0 + e];
-            if (in) x[e] = __builtin_fmaf(x[e], co, o * si);
+            const float co = cs[t][i0 + e], si = low ? -sn[t][i0 + e] : sn[t][i0 + e];
+            x[e] = __builtin_fmaf(x[e], co, o[e] * si);
           }
         }
-        w = pack_slice<DTYPE>(x);
       }
-      char* dst;
-      if (isq) {
-        dst = (char*)a.q_out + ((size_t)t * a.hq + h) * D * ELT;
-      } else if (a.k_out) {
-        dst = (char*)a.k_out + ((size_t)t * a.hk + h) * D * ELT;
-      } else {
-        const int u = (b * a.n_layers + a.layer) * a.hk + h;
-        dst = (char*)(isv ? a.vc : a.kc) +
-              ((size_t)u * a.cap + rows_before(a.unit_len, a.len, u) + r) * D * ELT;
-      }
-      if (isq || owned) *reinterpret_cast<uint4*>(dst + c * 16) = w;
+      x16 = pack_slice<DTYPE>(x);
     }
-    __syncthreads();
+    char* dst;
+    if (isq) {
+      dst = (char*)a.q_out + ((size_t)(first + t) * a.hq + h) * D * ELT;
+    } else if (a.k_out) {
+      dst = (char*)a.k_out + ((size_t)(first + t) * a.hk + h) * D * ELT;
+    } else {
+      const int u = (seq[t] * a.n_layers + a.layer) * a.hk + h;
+      if (num[t] < 0) return;
+      dst = (char*)(isv ? a.vc : a.kc) +
+            ((size_t)u * a.cap + rows_before(a.unit_len, a.len, u) + num[t]) * D * ELT;
+    }
+    *reinterpret_cast<uint4*>(dst + c * 16) = x16;
+  };
+  for (int i = 0; i < items; i += BATCH) {
+    uint4 y[BATCH];
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      y[x] = w[x];
+      w[x] = load(i + BATCH + x);
+    }
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) finish(i + x, y[x]);
   }
 }
 
@@ -224,9 +272,14 @@ __global__ void commit_len_kernel(CommitArgs a) {
 
 template <int DTYPE, int D>
 void norm_rope(const NormRopeArgs& a, hipStream_t s) {
-  const int per = a.tok.tokens >= 8192 ? 4 : 1;
-  hipLaunchKernelGGL((norm_rope_kernel<DTYPE, D>), dim3((a.tok.tokens + per - 1) / per), dim3(RT), 0, s, a,
-                     per);
+  constexpr int GROUPS = RT / RowT<DTYPE, D>::LPR;
+  const int nrows = a.hq + a.hk + (a.k_out ? 0 : a.hk), passes = (nrows + GROUPS - 1) / GROUPS;
+  const int64_t one = (int64_t)a.tok.tokens * passes;
+  if (one <= FEW_WGS)
+    hipLaunchKernelGGL((norm_rope_kernel<DTYPE, D, 1>), dim3(a.tok.tokens, passes), dim3(RT), 0, s, a, 1, 1);
+  else
+    hipLaunchKernelGGL((norm_rope_kernel<DTYPE, D, 2>), dim3((a.tok.tokens + TPB - 1) / TPB), dim3(RT), 0, s, a,
+                       TPB, passes);
 }
 
 template <int DTYPE, int D>
