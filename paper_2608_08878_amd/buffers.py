@@ -2,7 +2,6 @@
 streams only; no computation happens here)."""
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
@@ -66,6 +65,7 @@ class DecodeBuffers:
         self.ws = None
         self.ws_bytes = 0
         self._older_ws = []
+        self._device = self.k.get_device()
         if features:
             self.reserve_workspace(capacity)
 
@@ -182,17 +182,29 @@ class DecodeBuffers:
 
     # ---- several tokens at once: prompts and drafted tokens
 
+    # (the checks cost host time on calls of a few microseconds: plain comparisons)
+
     def _rows_of(self, x, heads, tokens, name):
         """x [N][heads][d] with dense rows: its elements from token to token."""
-        self._batch_of(tokens)
-        if x.dtype != self.k.dtype or tuple(x.shape) != (tokens.tokens, heads, self.D):
-            raise ValueError(f"{name} must be {self.k.dtype} [{tokens.tokens}][{heads}][{self.D}], "
-                             f"got {x.dtype} {list(x.shape)}")
-        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.D):
+        n, d = tokens.tokens, self.D
+        if x.dtype != self.k.dtype or x.shape != (n, heads, d):
+            raise ValueError(f"{name} must be {self.k.dtype} [{n}][{heads}][{d}], got {x.dtype} {list(x.shape)}")
+        ld, between, one = x.stride()
+        if one != 1 or (between != d and heads > 1):
             raise ValueError(f"{name}'s heads must be contiguous within a token")
         self._here(x, name)
-        # (a single token's stride is never used)
-        return x.stride(0) if tokens.tokens > 1 else heads * self.D
+        return ld if n > 1 else heads * d        # (a single token's stride is never used)
+
+    def _like(self, x, tokens, heads, name):
+        """An output given by the caller."""
+        if self._rows_of(x, heads, tokens, name) != heads * self.D:
+            raise ValueError(f"{name} must be contiguous")
+        return x
+
+    def _ints(self, x, shape, name):
+        if x.dtype != torch.int32 or x.shape != shape or not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous int32 {list(shape)}, got {x.dtype} {list(x.shape)}")
+        self._here(x, name)
 
     def _batch_of(self, tokens):
         n = getattr(tokens, "sequences", self.dims.batch)
@@ -200,46 +212,40 @@ class DecodeBuffers:
             raise ValueError(f"tokens of {n} sequences for a cache of {self.dims.batch}")
 
     def _here(self, x, name):
-        if x.device != self.k.device:
+        if x.get_device() != self._device:
             raise ValueError(f"{name} is on {x.device}, the cache on {self.k.device}")
 
     def _stream_here(self, stream):
         """The stream's handle; the cache has to be on the current device, which launches it."""
-        if self.k.device.index != torch.cuda.current_device():
+        if torch.cuda.current_device() != self._device:
             raise ValueError(f"the cache is on {self.k.device}, the current device is "
                              f"cuda:{torch.cuda.current_device()}")
         return stream_handle(stream)
 
     def _empty(self, shape, dtype, stream):
         """Memory that the given stream uses first (the allocator orders reuse by stream)."""
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        if stream is None:
             return torch.empty(shape, dtype=dtype, device=self.k.device)
-
-    def _ints(self, x, shape, name):
-        if x is not None and (x.dtype != torch.int32 or tuple(x.shape) != shape or not x.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous int32 {list(shape)}, got {x.dtype} {list(x.shape)}")
-        if x is not None:
-            self._here(x, name)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.k.device)
 
     def norm_rope(self, tokens, rope, q, k, v=None, pos=None, layer=0, q_out=None, k_out=None, stream=None):
         """Queries and keys of `tokens` normed and rotated (dc_qk_norm_rope).  With v the rotated
         keys and the values go into the cache behind its rows; without, the keys are
         returned too.  Returns (q_out, k_out or None)."""
         hq, hk = self.dims.n_q_heads, self.dims.n_kv_heads
+        self._batch_of(tokens)
         ld_q, ld_k = self._rows_of(q, hq, tokens, "q"), self._rows_of(k, hk, tokens, "k")
-        ld_v = self._rows_of(v, hk, tokens, "v") if v is not None else 0
-        self._ints(pos, (tokens.tokens,), "pos")
-        if q_out is None:
-            q_out = self._empty((tokens.tokens, hq, self.D), q.dtype, stream)
-        elif not q_out.is_contiguous() or q_out.shape != q.shape or q_out.dtype != q.dtype:
-            raise ValueError("q_out must be contiguous and like q")
+        if pos is not None:
+            self._ints(pos, (tokens.tokens,), "pos")
+        q_out = self._empty(q.shape, q.dtype, stream) if q_out is None else self._like(q_out, tokens, hq, "q_out")
+        ld_v = 0
         if v is not None:
             if k_out is not None:
                 raise ValueError("with v the keys go to the cache: no k_out")
-        elif k_out is None:
-            k_out = self._empty((tokens.tokens, hk, self.D), k.dtype, stream)
-        elif not k_out.is_contiguous() or k_out.shape != k.shape or k_out.dtype != k.dtype:
-            raise ValueError("k_out must be contiguous and like k")
+            ld_v = self._rows_of(v, hk, tokens, "v")
+        else:
+            k_out = self._empty(k.shape, k.dtype, stream) if k_out is None else self._like(k_out, tokens, hk, "k_out")
         B.dc_qk_norm_rope(self.dims, self.kv, layer, tokens, rope, q, ld_q, k, ld_k, v, ld_v, pos, q_out, k_out,
                           self._stream_here(stream))
         return q_out, k_out
@@ -252,14 +258,10 @@ class DecodeBuffers:
             self.ws_bytes = need
 
     def _check_queries(self, tokens, q, out, stream):
-        self._rows_of(q, self.dims.n_q_heads, tokens, "q")
-        if not q.is_contiguous():
-            raise ValueError("q must be contiguous")
-        if out is None:
-            return self._empty(q.shape, q.dtype, stream)
-        if not out.is_contiguous() or out.shape != q.shape or out.dtype != q.dtype:
-            raise ValueError("out must be contiguous and like q")
-        return out
+        self._batch_of(tokens)
+        hq = self.dims.n_q_heads
+        self._like(q, tokens, hq, "q")
+        return self._empty(q.shape, q.dtype, stream) if out is None else self._like(out, tokens, hq, "out")
 
     def prompt_attention(self, tokens, q, layer=0, out=None, stream=None):
         """Causal attention of packed prompts whose K/V are behind the cache's rows."""
@@ -286,7 +288,8 @@ class DecodeBuffers:
             self._ints(path, (self.dims.batch, width), "path")
         elif width is None:
             width = tokens.max_tokens
-        self._ints(keep, (self.dims.batch,), "keep")
+        if keep is not None:
+            self._ints(keep, (self.dims.batch,), "keep")
         B.dc_commit_rows(self.dims, self.kv, self.feat, tokens, path, keep, width, self._stream_here(stream))
 
     def prefill(self, tokens, rope, q, k, v, pos, layer=0, out=None, stream=None):

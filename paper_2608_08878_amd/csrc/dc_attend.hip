@@ -32,6 +32,8 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef short i16x8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_c_t;
 
+#define DC_INLINE __attribute__((always_inline))
+
 constexpr int MAX_NODES = DC_TREE_MAX_NODES;
 constexpr int MASK_WORDS = MAX_NODES / 32;
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -188,6 +190,126 @@ struct Cfg {
   static_assert(TILE % 1024 == 0 && SK % 32 == 0, "tile shape");
 };
 
+// Where a workgroup's row tile and keys are.
+struct Place {
+  int u, g, t0, n;              // unit, KV head, first packed token and tokens of the sequence
+  int start, total;             // rows before the tokens' own, and with them
+  int rows, row0;               // (token, head) rows, the tile's first
+  int split, k0, k1;            // the part of the keys: k0 .. k1 - 1
+};
+
+// One launch index per (row tile, key part, sequence and KV head), the pairs fastest: with a
+// multiple of 8 of them a pair's workgroups share one XCD's L2.  The tiles with the most keys
+// go first.  False where nothing is to be done (the whole workgroup).
+template <bool TREE>
+__device__ __forceinline__ bool locate(const AttendArgs& a, int bm, Place& w) {
+  const int pairs = a.batch * a.hk;
+  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int tile = a.ntiles - 1 - rest / a.splits;
+  const int b = pair / a.hk;
+  w.split = rest % a.splits;
+  w.g = pair % a.hk;
+  w.u = (b * a.n_layers + a.layer) * a.hk + w.g;
+  token_range(a.tok, b, w.t0, w.n);
+  w.t0 = __builtin_amdgcn_readfirstlane(w.t0);      // uniform, and known to be
+  w.n = __builtin_amdgcn_readfirstlane(w.n);
+  w.rows = w.n << a.gshift;
+  w.row0 = tile * bm;
+  if (w.row0 >= w.rows) return false;
+  w.start = __builtin_amdgcn_readfirstlane(rows_before(a.unit_len, a.len, w.u));
+  w.total = w.start + w.n;
+  const int last = (w.row0 + bm < w.rows ? w.row0 + bm : w.rows) - 1;
+  const int kend = TREE ? w.total : w.start + (last >> a.gshift) + 1;   // keys any row of the tile sees
+  w.k0 = w.split * a.chunk;
+  w.k1 = w.k0 + a.chunk < kend ? w.k0 + a.chunk : kend;
+  return w.k0 < w.k1;
+}
+
+// Ancestors of every node as bits (a node is its own), by doubling the step up the tree.  A parent
+// that is not an earlier node of the sequence counts as none.
+__device__ __forceinline__ void ancestors(const AttendArgs& a, const Place& w, uint32_t* anc, int* up) {
+  const int n = w.n, words = (n + 31) / 32, i = threadIdx.x;
+  if (i < n) {
+    const int p = a.parent[w.t0 + i];
+    up[i] = p >= 0 && p < i ? p : -1;
+    for (int x = 0; x < words; ++x) anc[i * MASK_WORDS + x] = x == i / 32 ? 1u << (i & 31) : 0u;
+  }
+  __syncthreads();
+  for (int step = 1; step < n; step *= 2) {
+    int p = -1;
+    uint32_t m[MASK_WORDS];
+    if (i < n && (p = up[i]) >= 0) {
+      for (int x = 0; x < words; ++x) m[x] = anc[p * MASK_WORDS + x];
+    }
+    const int pp = p >= 0 ? up[p] : -1;
+    __syncthreads();
+    if (p >= 0) {
+      for (int x = 0; x < words; ++x) anc[i * MASK_WORDS + x] |= m[x];
+      up[i] = pp;
+    }
+    __syncthreads();
+  }
+}
+
+// Which keys of the block kb .. kb + 31 token r sees.
+template <bool TREE>
+__device__ __forceinline__ uint32_t sees32(const Place& w, const uint32_t* anc, int r, int kb) {
+  if constexpr (TREE) {
+    const int d = kb - w.start;
+    if (d <= -32) return ~0u;
+    const uint32_t* m = anc + r * MASK_WORDS;
+    const int words = (w.n + 31) / 32;
+    if (d < 0) return m[0] << -d | ((1u << -d) - 1u);
+    const int x = d >> 5, s = d & 31;
+    const uint32_t lo = x < words ? m[x] : 0u, hi = x + 1 < words ? m[x + 1] : 0u;
+    return s ? lo >> s | hi << (32 - s) : lo;
+  } else {
+    const int nv = w.start + r + 1 - kb;
+    return nv >= 32 ? ~0u : nv <= 0 ? 0u : (1u << nv) - 1u;
+  }
+}
+
+// Scores of the keys that a lane's row does not see become minus infinity.
+__device__ __forceinline__ void mask32(f32x16_t& s, uint32_t sees, int h) {
+  sees >>= 4 * h;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = (sees >> (8 * (i / 4) + i % 4)) & 1 ? s[i] : NEG_INF;
+}
+
+// A lane's row of the output (l over all its keys), or of its key part's share.
+template <int DT, int D>
+__device__ __forceinline__ void store_row(const AttendArgs& a, size_t qrow, int split, const f32x16_t* o, float m,
+                                          float l, int h) {
+  if (a.splits > 1) {
+    float* po = a.part + (qrow * a.splits + split) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(po + 32 * db + 8 * q + 4 * h) =
+            make_float4(o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]);
+    if (h == 0)
+      *reinterpret_cast<float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D +
+                                 (qrow * a.splits + split) * 2) = make_float2(m, l);
+    return;
+  }
+  const float inv = 1.0f / l;
+  char* out = (char*)a.out + qrow * KVT<DT, D>::RB;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * db + 8 * q + 4 * h;
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = o[db][4 * q + e] * inv;
+      if constexpr (DT == 1)
+        *reinterpret_cast<uint2*>(out + d * 2) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+      else
+        *reinterpret_cast<float4*>(out + d * 4) = make_float4(f[0], f[1], f[2], f[3]);
+    }
+}
+
 template <int DT, int D, int RW, int KW, int SK, bool TREE>
 __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) attend_kernel(AttendArgs a) {
   using T = KVT<DT, D>;
@@ -198,100 +320,51 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
   const int lane = threadIdx.x & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rw = wave % RW, kw = wave / RW;
-  const int G = 1 << a.gshift;
-
-  // One launch index per (row tile, key part, sequence and KV head), the pairs fastest: with a
-  // multiple of 8 of them a pair's workgroups share one XCD's L2.  The tiles with the most keys
-  // go first.
-  const int pairs = a.batch * a.hk;
-  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int split = rest % a.splits, tile = a.ntiles - 1 - rest / a.splits;
-  const int b = pair / a.hk, g = pair % a.hk;
-  const int u = (b * a.n_layers + a.layer) * a.hk + g;
-  int t0, n;
-  token_range(a.tok, b, t0, n);
-  const int rows = n << a.gshift, row0 = tile * C::BM;
-  if (row0 >= rows) return;
-  const int start = rows_before(a.unit_len, a.len, u), total = start + n;
-  const int last = (row0 + C::BM < rows ? row0 + C::BM : rows) - 1;
-  const int kend = TREE ? total : start + (last >> a.gshift) + 1;   // keys any row of the tile sees
-  const int k0 = split * a.chunk;
-  const int k1 = k0 + a.chunk < kend ? k0 + a.chunk : kend;
-  if (k0 >= k1) return;
-
-  if constexpr (TREE) {
-    // Ancestors of every node as bits, by doubling the step up the tree.  A parent that is not an
-    // earlier node of the sequence counts as none.
-    const int words = (n + 31) / 32;
-    for (int i = threadIdx.x; i < n; i += C::THREADS) {
-      const int p = a.parent[t0 + i];
-      up[i] = p >= 0 && p < i ? p : -1;
-      for (int w = 0; w < words; ++w) anc[i * MASK_WORDS + w] = w == i / 32 ? 1u << (i & 31) : 0u;
-    }
-    __syncthreads();
-    static_assert(C::THREADS >= MAX_NODES, "a thread per node");
-    for (int step = 1; step < n; step *= 2) {
-      const int i = threadIdx.x;
-      int p = -1;
-      uint32_t m[MASK_WORDS];
-      if (i < n && (p = up[i]) >= 0) {
-        for (int w = 0; w < words; ++w) m[w] = anc[p * MASK_WORDS + w];
-      }
-      const int pp = p >= 0 ? up[p] : -1;
-      __syncthreads();
-      if (p >= 0) {
-        for (int w = 0; w < words; ++w) anc[i * MASK_WORDS + w] |= m[w];
-        up[i] = pp;
-      }
-      __syncthreads();
-    }
-  }
+  Place w;
+  if (!locate<TREE>(a, C::BM, w)) return;
+  static_assert(C::THREADS >= MAX_NODES, "a thread per node");
+  if constexpr (TREE) ancestors(a, w, anc, up);
 
   // this lane's row
-  const int wrow = row0 + 32 * rw;
-  const int myrow = wrow + (lane & 31) < rows ? wrow + (lane & 31) : rows - 1;
-  const int r = myrow >> a.gshift, head = (g << a.gshift) + (myrow & (G - 1));
-  const bool active = wrow < rows;
-  const size_t qrow = (size_t)(t0 + r) * a.hq + head;
+  const int wrow = w.row0 + 32 * rw;
+  const int myrow = wrow + (lane & 31) < w.rows ? wrow + (lane & 31) : w.rows - 1;
+  const int r = myrow >> a.gshift;
+  const bool active = wrow < w.rows;
+  const size_t qrow = (size_t)(w.t0 + r) * a.hq + (w.g << a.gshift) + (myrow & ((1 << a.gshift) - 1));
   uint4 qf[T::KT];
 #pragma unroll
   for (int t = 0; t < T::KT; ++t) qf[t] = ldg16((const char*)a.q + qrow * T::RB + (2 * t + h) * 16);
-  const int wfirst = (wrow < rows ? wrow : rows - 1) >> a.gshift;            // the wave's first token
-  const int wlast = (wrow + 31 < rows ? wrow + 31 : rows - 1) >> a.gshift;   // and its last
-  const int full = TREE ? start : start + wfirst + 1;   // keys below are seen by all its rows
-  const int some = TREE ? total : start + wlast + 1;    // keys from here on by none
+  const int wfirst = (wrow < w.rows ? wrow : w.rows - 1) >> a.gshift;            // the wave's first token
+  const int wlast = (wrow + 31 < w.rows ? wrow + 31 : w.rows - 1) >> a.gshift;   // and its last
+  const int full = TREE ? w.start : w.start + wfirst + 1;   // keys below are seen by all its rows
+  const int some = TREE ? w.total : w.start + wlast + 1;    // keys from here on by none
+  const int k0 = w.k0, k1 = w.k1, total = w.total;
 
-  // which keys of the block kb .. kb + 31 this lane's row sees
-  auto sees32 = [&](int kb) -> uint32_t {
-    if constexpr (TREE) {
-      const int d = kb - start;
-      if (d <= -32) return ~0u;
-      const uint32_t* m = anc + r * MASK_WORDS;
-      const int words = (n + 31) / 32;
-      if (d < 0) return m[0] << -d | ((1u << -d) - 1u);
-      const int w = d >> 5, s = d & 31;
-      const uint32_t lo = w < words ? m[w] : 0u, hi = w + 1 < words ? m[w + 1] : 0u;
-      return s ? lo >> s | hi << (32 - s) : lo;
-    } else {
-      const int nv = start + r + 1 - kb;
-      return nv >= 32 ? ~0u : nv <= 0 ? 0u : (1u << nv) - 1u;
-    }
-  };
-
-  // tile loads: 1024 bytes an instruction, the waves in turn
-  const char* kc = (const char*)a.k + (size_t)u * a.cap * T::RB;
-  const char* vc = (const char*)a.v + (size_t)u * a.cap * T::RB;
+  // tile loads: 1024 bytes an instruction, the waves in turn; rows past the last are read as the last
+  constexpr int LPW = C::TILE / 1024 / C::NW, RPI = 1024 / T::RB;    // instructions of a wave, rows of one
+  const char* kc = (const char*)a.k + ((size_t)w.u * a.cap + k0) * T::RB;
+  const char* vc = (const char*)a.v + ((size_t)w.u * a.cap + k0) * T::RB;
   const uint32_t lds0 = lds_offset(lds);
-  auto load_tile = [&](int kb, int buf) {
-    constexpr int RPI = 1024 / T::RB;            // rows an instruction covers
+  uint32_t ko[LPW], vo[LPW];
 #pragma unroll
-    for (int x = 0; x < C::TILE / 1024 / C::NW; ++x) {
-      const int i = x * C::NW + wave;
-      const int row = i * RPI + lane / T::CH, p = lane % T::CH;
-      const int src = kb + row < total ? kb + row : total - 1;
-      load_to_lds16(kc + (size_t)src * T::RB + (p ^ T::kx(row)) * 16, lds0 + buf * C::BUF + i * 1024);
-      load_to_lds16(vc + (size_t)src * T::RB + (p ^ T::vx(row)) * 16,
-                    lds0 + buf * C::BUF + C::TILE + i * 1024);
+  for (int x = 0; x < LPW; ++x) {
+    const int row = (x * C::NW + wave) * RPI + lane / T::CH, p = lane % T::CH;
+    ko[x] = row * T::RB + (p ^ T::kx(row)) * 16;
+    vo[x] = row * T::RB + (p ^ T::vx(row)) * 16;
+  }
+  auto load_tile = [&](int it, int buf) DC_INLINE {
+    const size_t at = (size_t)it * C::TILE;
+    const int left = total - k0 - it * C::BN;
+#pragma unroll
+    for (int x = 0; x < LPW; ++x) {
+      uint32_t back = 0;
+      if (left < C::BN) {
+        const int row = (x * C::NW + wave) * RPI + lane / T::CH;
+        if (row >= left) back = (row - left + 1) * T::RB;
+      }
+      const uint32_t dst = lds0 + buf * C::BUF + (x * C::NW + wave) * 1024;
+      load_to_lds16_at(kc + at, ko[x] - back, dst);
+      load_to_lds16_at(vc + at, vo[x] - back, dst + C::TILE);
     }
   };
 
@@ -300,19 +373,19 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
   float m, l;
   const int ntile = (k1 - k0 + C::BN - 1) / C::BN;
   // One pass over the keys.  CAREFUL: masked blocks go key by key.
-  auto pass = [&](auto careful) {
+  auto pass = [&](auto careful) DC_INLINE {
     constexpr bool CAREFUL = decltype(careful)::value;
     m = NEG_INF;
     l = 0.0f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16_t{};
     // a tile in buffer BUF; the next one's loads are under way meanwhile
-    auto tile_step = [&](int it, auto bufc) {
+    auto tile_step = [&](int it, auto bufc) DC_INLINE {
       constexpr int BUF = decltype(bufc)::value;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       const int kt = k0 + it * C::BN;
-      if (it + 1 < ntile) load_tile(kt + C::BN, 1 - BUF);
+      if (it + 1 < ntile) load_tile(it + 1, 1 - BUF);
       const int kb = kt + kw * SK;
       if (!active || kb >= k1 || kb >= some) return;
       const char* kl = lds + BUF * C::BUF + kw * SK * T::RB;
@@ -323,14 +396,15 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
 #pragma unroll
       for (int x = 0; x < SK / 32; ++x) {
         s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
-        if (masked) {
-          const uint32_t w = sees32(kb + 32 * x) >> (4 * h);
+      }
+      if (masked) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[x][i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[x][i] : NEG_INF;
-        }
+        for (int x = 0; x < SK / 32; ++x) mask32(s[x], sees32<TREE>(w, anc, r, kb + 32 * x), h);
+      }
+#pragma unroll
+      for (int x = 0; x < SK / 32; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
-      }
       const float mn = fmaxf(m, half_max(mx) * c);
       if (__any(mn > m + SLACK)) {
         const float f = rescale(m, mn);
@@ -349,11 +423,11 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
           s[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], c, -mc));
           l += s[x][i];
         }
-        if (CAREFUL && masked) values32_masked<DT, D>(vl + 32 * x * T::RB, s[x], sees32(kb + 32 * x), o, lane);
+        if (CAREFUL && masked) values32_masked<DT, D>(vl + 32 * x * T::RB, s[x], sees32<TREE>(w, anc, r, kb + 32 * x), o, lane);
         else values32<DT, D>(vl + 32 * x * T::RB, s[x], o, lane);
       }
     };
-    load_tile(k0, 0);
+    load_tile(0, 0);
     for (int it = 0; it < ntile; it += 2) {
       tile_step(it, std::integral_constant<int, 0>{});
       if (it + 1 < ntile) tile_step(it + 1, std::integral_constant<int, 1>{});
@@ -412,37 +486,7 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
     }
     m = mm;
   }
-  if (wrow + (lane & 31) >= rows) return;
-  if (a.splits > 1) {
-    float* po = a.part + (qrow * a.splits + split) * D;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4*>(po + 32 * db + 8 * q + 4 * h) =
-            make_float4(o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]);
-    if (h == 0)
-      *reinterpret_cast<float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D +
-                                 (qrow * a.splits + split) * 2) = make_float2(m, l);
-    return;
-  }
-  const float inv = 1.0f / l;
-  char* out = (char*)a.out + qrow * T::RB;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int d = 32 * db + 8 * q + 4 * h;
-      float f[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[e] = o[db][4 * q + e] * inv;
-      if constexpr (DT == 1)
-        *reinterpret_cast<uint2*>(out + d * 2) =
-            make_uint2(f32_to_bf16_bits(f[0]) | f32_to_bf16_bits(f[1]) << 16,
-                       f32_to_bf16_bits(f[2]) | f32_to_bf16_bits(f[3]) << 16);
-      else
-        *reinterpret_cast<float4*>(out + d * 4) = make_float4(f[0], f[1], f[2], f[3]);
-    }
+  if (wrow + (lane & 31) < w.rows) store_row<DT, D>(a, qrow, w.split, o, m, l, h);
 }
 
 // Joins the parts of the key range, a wave per row.

@@ -38,6 +38,12 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
   return (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
 }
 
+// Two float32 numbers rounded to bf16 (to nearest even, NaN kept) in one instruction.
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
+}
+
 // Partial dot product of the lane's 16-byte slices (fixed evaluation order).
 template <int DTYPE>
 __device__ __forceinline__ float dot_slice(const uint4& q, const uint4& k) {
@@ -184,6 +190,12 @@ __device__ __forceinline__ void compiler_fence() { asm volatile("" ::: "memory")
 __device__ __forceinline__ void load_to_lds16(const void* g, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                : : "v"(g), "s"(lds) : "memory", "m0");
+}
+
+// The same from byte voff of a uniform address: no vector instruction advances it.
+__device__ __forceinline__ void load_to_lds16_at(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               : : "v"(voff), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 }  // namespace dc

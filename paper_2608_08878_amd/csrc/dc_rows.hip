@@ -14,12 +14,6 @@ constexpr int RT = 256;               // threads of a workgroup
 constexpr int MAX_PAIRS = 64;         // rotated pairs of a head of 128
 constexpr double INV_2PI = 0.15915494309189533577;
 
-// Two float32 numbers rounded to bf16 (to nearest even, NaN kept) in one instruction.
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
-}
-
 template <int DTYPE>
 __device__ __forceinline__ uint4 pack_slice(const float* f) {
   if constexpr (DTYPE == 1)
