@@ -186,6 +186,8 @@ struct Cfg {
   static constexpr int BUF = 2 * TILE;
   static constexpr int OB = 32 * D * 4 + 256;             // one wave's partial result
   static constexpr int LDS = 2 * BUF;
+  // workgroups of a CU by their LDS; their waves on a SIMD
+  static constexpr int WAVES = 2 * LDS <= 144 * 1024 && NW == 4 ? 2 : 1;
   static_assert((KW - 1) * RW * OB <= LDS, "partials fit the tile buffers");
   static_assert(TILE % 1024 == 0 && SK % 32 == 0, "tile shape");
 };
@@ -227,25 +229,36 @@ __device__ __forceinline__ bool locate(const AttendArgs& a, int bm, Place& w) {
 
 // Ancestors of every node as bits (a node is its own), by doubling the step up the tree.  A parent
 // that is not an earlier node of the sequence counts as none.
+template <int THREADS>
 __device__ __forceinline__ void ancestors(const AttendArgs& a, const Place& w, uint32_t* anc, int* up) {
-  const int n = w.n, words = (n + 31) / 32, i = threadIdx.x;
-  if (i < n) {
+  constexpr int PER = (MAX_NODES + THREADS - 1) / THREADS;       // nodes of a thread
+  const int n = w.n, words = (n + 31) / 32;
+  for (int i = threadIdx.x; i < n; i += THREADS) {
     const int p = a.parent[w.t0 + i];
     up[i] = p >= 0 && p < i ? p : -1;
     for (int x = 0; x < words; ++x) anc[i * MASK_WORDS + x] = x == i / 32 ? 1u << (i & 31) : 0u;
   }
   __syncthreads();
   for (int step = 1; step < n; step *= 2) {
-    int p = -1;
-    uint32_t m[MASK_WORDS];
-    if (i < n && (p = up[i]) >= 0) {
-      for (int x = 0; x < words; ++x) m[x] = anc[p * MASK_WORDS + x];
+    uint32_t m[PER][MASK_WORDS];
+    int p[PER], pp[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      p[k] = i < n ? up[i] : -1;
+      pp[k] = p[k] >= 0 ? up[p[k]] : -1;
+#pragma unroll
+      for (int x = 0; x < MASK_WORDS; ++x) m[k][x] = p[k] >= 0 && x < words ? anc[p[k] * MASK_WORDS + x] : 0u;
     }
-    const int pp = p >= 0 ? up[p] : -1;
     __syncthreads();
-    if (p >= 0) {
-      for (int x = 0; x < words; ++x) anc[i * MASK_WORDS + x] |= m[x];
-      up[i] = pp;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      if (p[k] < 0) continue;
+      up[i] = pp[k];
+#pragma unroll
+      for (int x = 0; x < MASK_WORDS; ++x)
+        if (x < words) anc[i * MASK_WORDS + x] |= m[k][x];
     }
     __syncthreads();
   }
@@ -311,7 +324,7 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, size_t qrow, int 
 }
 
 template <int DT, int D, int RW, int KW, int SK, bool TREE>
-__global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES)) attend_kernel(AttendArgs a) {
   using T = KVT<DT, D>;
   using C = Cfg<DT, D, RW, KW, SK>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -322,24 +335,7 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
   const int rw = wave % RW, kw = wave / RW;
   Place w;
   if (!locate<TREE>(a, C::BM, w)) return;
-  static_assert(C::THREADS >= MAX_NODES, "a thread per node");
-  if constexpr (TREE) ancestors(a, w, anc, up);
-
-  // this lane's row
-  const int wrow = w.row0 + 32 * rw;
-  const int myrow = wrow + (lane & 31) < w.rows ? wrow + (lane & 31) : w.rows - 1;
-  const int r = myrow >> a.gshift;
-  const bool active = wrow < w.rows;
-  const size_t qrow = (size_t)(w.t0 + r) * a.hq + (w.g << a.gshift) + (myrow & ((1 << a.gshift) - 1));
-  uint4 qf[T::KT];
-#pragma unroll
-  for (int t = 0; t < T::KT; ++t) qf[t] = ldg16((const char*)a.q + qrow * T::RB + (2 * t + h) * 16);
-  const int wfirst = (wrow < w.rows ? wrow : w.rows - 1) >> a.gshift;            // the wave's first token
-  const int wlast = (wrow + 31 < w.rows ? wrow + 31 : w.rows - 1) >> a.gshift;   // and its last
-  const int full = TREE ? w.start : w.start + wfirst + 1;   // keys below are seen by all its rows
-  const int some = TREE ? w.total : w.start + wlast + 1;    // keys from here on by none
   const int k0 = w.k0, k1 = w.k1, total = w.total;
-
   // tile loads: 1024 bytes an instruction, the waves in turn; rows past the last are read as the last
   constexpr int LPW = C::TILE / 1024 / C::NW, RPI = 1024 / T::RB;    // instructions of a wave, rows of one
   const char* kc = (const char*)a.k + ((size_t)w.u * a.cap + k0) * T::RB;
@@ -367,6 +363,22 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
       load_to_lds16_at(vc + at, vo[x] - back, dst + C::TILE);
     }
   };
+  load_tile(0, 0);        // under way while the rest is set up
+
+  // this lane's row
+  const int wrow = w.row0 + 32 * rw;
+  const int myrow = wrow + (lane & 31) < w.rows ? wrow + (lane & 31) : w.rows - 1;
+  const int r = myrow >> a.gshift;
+  const bool active = wrow < w.rows;
+  const size_t qrow = (size_t)(w.t0 + r) * a.hq + (w.g << a.gshift) + (myrow & ((1 << a.gshift) - 1));
+  uint4 qf[T::KT];
+#pragma unroll
+  for (int t = 0; t < T::KT; ++t) qf[t] = ldg16((const char*)a.q + qrow * T::RB + (2 * t + h) * 16);
+  const int wfirst = (wrow < w.rows ? wrow : w.rows - 1) >> a.gshift;            // the wave's first token
+  const int wlast = (wrow + 31 < w.rows ? wrow + 31 : w.rows - 1) >> a.gshift;   // and its last
+  const int full = TREE ? w.start : w.start + wfirst + 1;   // keys below are seen by all its rows
+  const int some = TREE ? w.total : w.start + wlast + 1;    // keys from here on by none
+  if constexpr (TREE) ancestors<C::THREADS>(a, w, anc, up);
 
   const float c = a.scale * LOG2E;
   f32x16_t o[D / 32];
@@ -427,7 +439,7 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
         else values32<DT, D>(vl + 32 * x * T::RB, s[x], o, lane);
       }
     };
-    load_tile(0, 0);
+    if (CAREFUL) load_tile(0, 0);
     for (int it = 0; it < ntile; it += 2) {
       tile_step(it, std::integral_constant<int, 0>{});
       if (it + 1 < ntile) tile_step(it + 1, std::integral_constant<int, 1>{});
@@ -489,7 +501,8 @@ __global__ void __launch_bounds__(64 * RW * KW, DT == 0 && D == 128 ? 1 : 2) att
   if (wrow + (lane & 31) < w.rows) store_row<DT, D>(a, qrow, w.split, o, m, l, h);
 }
 
-// Joins the parts of the key range, a wave per row.
+// Joins the parts of the key range, a wave per row: lane x holds part x's maximum and sum, then the
+// wave adds the parts' outputs, eight loads under way.
 template <int DT, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   constexpr int EPL = D / 64;
@@ -503,32 +516,46 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   if (row >= n << a.gshift) return;
   const int r = row >> a.gshift, head = (g << a.gshift) + (row & ((1 << a.gshift) - 1));
   const int keys = rows_before(a.unit_len, a.len, u) + (a.parent ? n : r + 1);
-  const int parts = (keys + a.chunk - 1) / a.chunk;       // those that a kernel wrote
+  const int parts = (keys + a.chunk - 1) / a.chunk;       // those that a kernel wrote: at most MAX_PARTS
   const size_t qrow = (size_t)(t0 + r) * a.hq + head;
-  const float* po = a.part + qrow * a.splits * D;
-  const float* ml = a.part + (size_t)a.tok.tokens * a.hq * a.splits * D + qrow * a.splits * 2;
-  float m = NEG_INF;
-  for (int s = 0; s < parts; ++s) m = fmaxf(m, ml[2 * s]);
-  float l = 0.0f, o[EPL] = {};
-  for (int s = 0; s < parts; ++s) {
-    const float f = rescale(ml[2 * s], m);
-    l = __builtin_fmaf(ml[2 * s + 1], f, l);
+  const float* po = a.part + qrow * a.splits * D + lane * EPL;
+  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D) +
+                     qrow * a.splits;
+  const float2 mine = lane < parts ? ml[lane] : make_float2(NEG_INF, 0.0f);
+  float m = mine.x;
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(po[(size_t)s * D + lane * EPL + e], f, o[e]);
+  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  const float f = lane < parts ? rescale(mine.x, m) : 0.0f;
+  float l = mine.y * f, o[EPL] = {};
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
+  for (int s = 0; s < parts; s += 8) {
+    float v[8][EPL];
+#pragma unroll
+    for (int y = 0; y < 8; ++y)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) v[y][e] = s + y < parts ? po[(size_t)(s + y) * D + e] : 0.0f;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const float fy = __shfl(f, s + y);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(v[y][e], fy, o[e]);
+    }
   }
   const float inv = 1.0f / l;
+  const size_t at = qrow * D + lane * EPL;
+  if constexpr (DT == 1 && EPL == 2)
+    reinterpret_cast<uint32_t*>(a.out)[at / 2] = pack_bf16(o[0] * inv, o[1] * inv);
+  else if constexpr (DT == 1)
+    reinterpret_cast<uint16_t*>(a.out)[at] = (uint16_t)f32_to_bf16_bits(o[0] * inv);
+  else
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) {
-    if constexpr (DT == 1)
-      reinterpret_cast<uint16_t*>(a.out)[qrow * D + lane * EPL + e] = (uint16_t)f32_to_bf16_bits(o[e] * inv);
-    else
-      reinterpret_cast<float*>(a.out)[qrow * D + lane * EPL + e] = o[e] * inv;
-  }
+    for (int e = 0; e < EPL; ++e) reinterpret_cast<float*>(a.out)[at + e] = o[e] * inv;
 }
 
 constexpr int CUS = 256;
-constexpr int FEW_ROWS = 32;         // rows of a sequence and KV head that one wave holds
-constexpr int MIN_CHUNK = 256;       // keys of a part, at least; a multiple of every key tile
+constexpr int MIN_CHUNK = 128;       // keys of a part, at least; a multiple of every key tile
+constexpr int MAX_PARTS = 64;        // of a key range: a lane each in the joining kernel
 
 template <int DT, int D, int RW, int KW, int SK>
 int launch_cfg(const AttendArgs& a, hipStream_t s) {
@@ -546,18 +573,16 @@ int launch_cfg(const AttendArgs& a, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
-// (float32 tiles of four key groups would not fit the LDS)
-bool few_rows(const AttendArgs& a, int dtype) {
-  return dtype == 1 && (int64_t)a.tok.max_tokens << a.gshift <= FEW_ROWS;
-}
-
+// Row tiles of 32 rows with the keys cut among the waves, of 64 and two groups, or of 128 rows.
+// (float32 tiles of 32 rows of 128 elements: two key groups; what four need does not fit the LDS)
 template <int DT, int D>
 int launch_type(const AttendArgs& a, hipStream_t s) {
   int rc;
   if constexpr (DT == 1)
-    rc = few_rows(a, DT) ? launch_cfg<DT, D, 1, 4, 32>(a, s) : launch_cfg<DT, D, 4, 1, 64>(a, s);
+    rc = a.bm == 32 ? launch_cfg<DT, D, 1, 4, 32>(a, s) : a.bm == 64 ? launch_cfg<DT, D, 2, 2, 64>(a, s)
+                                                                     : launch_cfg<DT, D, 4, 1, 64>(a, s);
   else
-    rc = launch_cfg<DT, D, 4, 1, 32>(a, s);
+    rc = a.bm == 32 ? launch_cfg<DT, D, 1, D == 64 ? 4 : 2, 32>(a, s) : launch_cfg<DT, D, 4, 1, 32>(a, s);
   if (rc == 0 && a.splits > 1) {
     const int64_t rows = (int64_t)a.tok.max_tokens << a.gshift;
     hipLaunchKernelGGL((attend_join_kernel<DT, D>), dim3((unsigned)(a.batch * a.hk * ((rows + 3) / 4))),
@@ -571,16 +596,24 @@ int launch_type(const AttendArgs& a, hipStream_t s) {
 
 bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   const int64_t rows = (int64_t)a.tok.max_tokens << a.gshift;
-  const int bm = few_rows(a, dtype) ? 32 : 128;
   const int64_t pairs = (int64_t)a.batch * a.hk;
-  const int64_t nt = (rows + bm - 1) / bm;
-  // row tiles in all: the packed tokens' and a part of one for every sequence
-  const int64_t all = ((int64_t)a.tok.tokens << a.gshift) * a.hk / bm + pairs;
-  const int64_t wgs = all < nt * pairs ? all : nt * pairs;
-  int64_t splits = 2 * CUS / wgs;
-  const int64_t most = (L + MIN_CHUNK - 1) / MIN_CHUNK;
-  splits = splits > most ? most : splits < 1 ? 1 : splits;
+  // workgroups of bm rows: the packed tokens' and a part of one for every sequence
+  auto tiles = [&](int bm) {
+    const int64_t all = ((int64_t)a.tok.tokens << a.gshift) * a.hk / bm + pairs, nt = (rows + bm - 1) / bm;
+    return all < nt * pairs ? all : nt * pairs;
+  };
+  const int64_t parts = (L + MIN_CHUNK - 1) / MIN_CHUNK;
+  int bm = 128;
+  if (rows <= 32 || tiles(128) * parts < CUS) bm = 32;
+  else if (rows <= 64 && dtype == 1) bm = 64;
+  // parts for every workgroup that the CUs hold at a time
+  const int per_cu = bm == 128 || (dtype == 1 && D == 64) ? 2 : 1;
+  int64_t splits = per_cu * CUS / tiles(bm);
+  splits = splits > parts ? parts : splits;
+  splits = splits > MAX_PARTS ? MAX_PARTS : splits < 1 ? 1 : splits;
   const int64_t chunk = ((L + splits - 1) / splits + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK;
+  const int64_t nt = (rows + bm - 1) / bm;
+  a.bm = bm;
   a.splits = (int)splits;
   a.chunk = (int)chunk;
   a.ntiles = (int)nt;

@@ -189,6 +189,7 @@ struct AttendArgs {
   int splits;               // parts of the key range, `chunk` rows each
   int chunk;
   int ntiles;               // row tiles of the longest sequence
+  int bm;                   // rows of a tile
 };
 
 // The rows behind each unit's length become part of the cache (dc_rows.hip).
