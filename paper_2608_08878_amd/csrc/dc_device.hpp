@@ -174,6 +174,21 @@ __device__ __forceinline__ void token_range(const TokenArgs& t, int b, int& t0, 
   n = t1 - t0 < t.max_tokens ? t1 - t0 : t.max_tokens;
 }
 
+// The sequence of packed token t: the last b with cu[b] <= t of the ascending offsets, found by the
+// wave together, 64 offsets a step (all its lanes take part, with the same t).
+__device__ __forceinline__ int sequence_of(const TokenArgs& tok, int batch, int t) {
+  if (!tok.cu) return t / tok.max_tokens;
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 1; b0 < batch; b0 += 64) {
+    const int b = b0 + lane;
+    const uint64_t m = __ballot(b < batch && tok.cu[b < batch ? b : 0] <= t);
+    before += __popcll(m);
+    if (m != ~0ull) break;
+  }
+  return before;
+}
+
 // Rows of unit u before a call's own (len: their bound).
 __device__ __forceinline__ int rows_before(const int32_t* unit_len, int len, int u) {
   if (!unit_len) return len;
@@ -195,6 +210,11 @@ __device__ __forceinline__ void load_to_lds16(const void* g, uint32_t lds) {
 // The same from byte voff of a uniform address: no vector instruction advances it.
 __device__ __forceinline__ void load_to_lds16_at(const void* base, uint32_t voff, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               : : "v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+}
+
+__device__ __forceinline__ void load_to_lds16_at_nt(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
                : : "v"(voff), "s"(base), "s"(lds) : "memory", "m0");
 }
 

@@ -190,6 +190,7 @@ struct AttendArgs {
   int chunk;
   int ntiles;               // row tiles of the longest sequence
   int bm;                   // rows of a tile
+  int once;                 // 1: K/V rows are read once, by non-temporal loads
 };
 
 // The rows behind each unit's length become part of the cache (dc_rows.hip).

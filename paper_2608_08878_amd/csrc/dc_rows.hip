@@ -38,7 +38,7 @@ __device__ __forceinline__ uint4 pack_slice(const float* f) {
 // places cost about 2 us of latency before its first store (16k tokens 437 us one at a time).
 // 20001 tokens of 32 + 16 heads of 128, 481 MB: 127 us = 3.8 TB/s, of the 4.8 that a copy reaches;
 // plain loads 138, three rows in flight 138 (fewer waves fit), tokens by two 157.
-constexpr int TPB = 4;
+constexpr int TPB = 4;               // (a wave each for their places)
 constexpr int FEW_WGS = 4096;
 
 template <int DTYPE, int D, int BATCH>
@@ -74,24 +74,16 @@ __global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_b
     const double turns = (double)a.pos[first + t] * (double)a.inv_freq[p] * INV_2PI;
     sincospif((float)(2.0 * (turns - rint(turns))), &sn[t][p], &cs[t][p]);
   }
-  if (!a.k_out && tid < count) {
-    const int t = first + tid;
-    int b = 0, r;
-    if (a.tok.cu) {
-      int lo = 0, hi = a.batch;             // the last b with cu[b] <= t
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.tok.cu[mid] <= t) lo = mid; else hi = mid;
-      }
-      b = lo;
-    } else {
-      b = t / a.tok.max_tokens;
+  if (!a.k_out) {             // a token per wave
+    const int x = tid >> 6;
+    if (x < count) {
+      const int b = sequence_of(a.tok, a.batch, first + x);
+      int t0, n;
+      token_range(a.tok, b, t0, n);
+      const int r = first + x - t0;
+      seq[x] = b;
+      num[x] = r >= 0 && r < n ? r : -1;
     }
-    int t0, n;
-    token_range(a.tok, b, t0, n);
-    r = t - t0;
-    seq[tid] = b;
-    num[tid] = r >= 0 && r < n ? r : -1;
   }
   float gq[EPL], gk[EPL];
 #pragma unroll
@@ -218,7 +210,7 @@ __global__ void __launch_bounds__(RT) commit_path_kernel(CommitArgs a) {
   for (int j0 = 0; j0 < keep; j0 += RPP) {
     const int j = j0 + jr;
     const bool on = j < keep;
-    int src = on ? a.path[(size_t)b * a.width + j] : 0;
+    int src = j < a.width ? a.path[(size_t)b * a.width + j] : 0;
     src = src < j ? j : src >= n ? n - 1 : src;
     const size_t from = (((size_t)u * a.cap + start + src) * LPR + c) * 16;
     const size_t to = (((size_t)u * a.cap + start + j) * LPR + c) * 16;
