@@ -187,8 +187,8 @@ struct Cfg {
   static constexpr int OB = 32 * D * 4 + 256;             // one wave's partial result
   static constexpr int LDS = 2 * BUF;
   // workgroups of a CU by their LDS; their waves on a SIMD
-  static constexpr int WAVES = 2 * LDS <= 144 * 1024 && NW == 4 ? 2 : 1;
-  static_assert((KW - 1) * RW * OB <= LDS, "partials fit the tile buffers");
+  static constexpr int WAVES = 2 * LDS <= 144 * 1024 && NW == 4 && !(DT == 0 && D == 128) ? 2 : 1;
+  static_assert((KW - 1) * RW * OB <= LDS && RW * 128 * D <= LDS, "results fit the tile buffers");
   static_assert(TILE % 1024 == 0 && SK % 32 == 0, "tile shape");
 };
 
@@ -321,6 +321,54 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, size_t qrow, int 
       else
         *reinterpret_cast<float4*>(out + d * 4) = make_float4(f[0], f[1], f[2], f[3]);
     }
+}
+
+// The same of the wave's 32 rows.  A lane holds pieces of 16 bytes of one row; they cross LDS (`st`, 128 D bytes of the wave's own, chunk c
+// of row r at c ^ r) so that the stores are whole rows
+// (16 prompts of up to 255 tokens 24.0 -> 20.6 us; a call of few rows, whose latency counts, is faster
+// without: 512 float32 tokens 12.2, with 12.9).
+template <int DT, int D>
+__device__ __forceinline__ void store_rows(const AttendArgs& a, const Place& w, int wrow, char* st, const f32x16_t* o,
+                                           float m, float l, int lane) {
+  constexpr int CH = D / 4;                       // chunks of four floats of a row
+  const int q = lane & 31, h = lane >> 5;
+  const bool parts = a.splits > 1;
+  const float inv = parts ? 1.0f : 1.0f / l;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      *reinterpret_cast<float4*>(st + (q * CH + ((8 * db + 2 * y + h) ^ (q & (CH - 1)))) * 16) =
+          make_float4(o[db][4 * y] * inv, o[db][4 * y + 1] * inv, o[db][4 * y + 2] * inv, o[db][4 * y + 3] * inv);
+  auto chunk = [&](int r, int c) DC_INLINE {
+    return *reinterpret_cast<const float4*>(st + (r * CH + (c ^ (r & (CH - 1)))) * 16);
+  };
+  auto place = [&](int row) DC_INLINE -> size_t {
+    return (size_t)(w.t0 + (row >> a.gshift)) * a.hq + (w.g << a.gshift) + (row & ((1 << a.gshift) - 1));
+  };
+  if (DT == 0 || parts) {
+    float* to = parts ? a.part : (float*)a.out;
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+      const int r = i * (64 / CH) + lane / CH, c = lane % CH;
+      if (wrow + r < w.rows) {
+        const size_t at = parts ? place(wrow + r) * a.splits + w.split : place(wrow + r);
+        *reinterpret_cast<float4*>(to + at * D + c * 4) = chunk(r, c);
+      }
+    }
+    if (parts && h == 0 && wrow + q < w.rows)
+      reinterpret_cast<float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D)[place(wrow + q) * a.splits +
+                                                                                    w.split] = make_float2(m, l);
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH / 4; ++i) {
+      const int r = i * (128 / CH) + lane / (CH / 2), c = lane % (CH / 2);
+      const float4 x = chunk(r, 2 * c), y = chunk(r, 2 * c + 1);
+      if (wrow + r < w.rows)
+        *reinterpret_cast<uint4*>((char*)a.out + place(wrow + r) * (2 * D) + c * 16) =
+            make_uint4(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w), pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    }
+  }
 }
 
 template <int DT, int D, int RW, int KW, int SK, bool TREE>
@@ -502,7 +550,11 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
     }
     m = mm;
   }
-  if (wrow + (lane & 31) < w.rows) store_row<DT, D>(a, qrow, w.split, o, m, l, h);
+  if constexpr (KW > 1) {
+    if (wrow + (lane & 31) < w.rows) store_row<DT, D>(a, qrow, w.split, o, m, l, h);
+  } else if (active) {
+    store_rows<DT, D>(a, w, wrow, lds + rw * 128 * D, o, m, l, lane);
+  }
 }
 
 // Joins the parts of the key range, a wave per row: lane x holds part x's maximum and sum, then the
