@@ -493,7 +493,7 @@ dc_status dc_reinforce_terms(int32_t steps, int32_t rollouts, const dc_reinforce
  * A sequence may have none.  Offsets on the device that are not ascending in
  * [0, tokens], or counts over max_tokens, are clamped. */
 typedef struct {
-  int32_t tokens;       /* N, at least 1 */
+  int32_t tokens;       /* N, 1 .. 2^25 */
   int32_t max_tokens;   /* host: the most tokens of one sequence (1..tokens) */
   const int32_t *cu;    /* device [batch + 1], or NULL: max_tokens each (tokens =
                            batch * max_tokens) */
@@ -542,7 +542,8 @@ dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
  * Slots that a token does not see have no influence on it, whatever they hold.
  * Workspace: dc_tokens_workspace_bytes(dims, tokens, kv->len + max_tokens) bytes.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_CAPACITY, DC_ERR_WORKSPACE,
- * DC_ERR_UNSUPPORTED (alignment, grids past 2^31 workgroups). */
+ * DC_ERR_UNSUPPORTED (alignment, grids past 2^24 workgroups: batch x KV heads x tiles of
+ * 32 to 128 (token, head) rows of the longest sequence). */
 dc_status dc_prompt_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer,
                               const dc_tokens *tokens, const void *q, void *out, void *ws,
                               size_t ws_bytes, void *hip_stream);

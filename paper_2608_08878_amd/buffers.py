@@ -222,12 +222,13 @@ class DecodeBuffers:
                              f"cuda:{torch.cuda.current_device()}")
         return stream_handle(stream)
 
-    def _empty(self, shape, dtype, stream):
-        """Memory that the given stream uses first (the allocator orders reuse by stream)."""
+    def _empty(self, shape, stream):
+        """A tensor of the cache's type in memory that the given stream uses first (the allocator
+        orders reuse by stream)."""
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.k.device)
+            return self.k.new_empty(shape)
         with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=self.k.device)
+            return self.k.new_empty(shape)
 
     def norm_rope(self, tokens, rope, q, k, v=None, pos=None, layer=0, q_out=None, k_out=None, stream=None):
         """Queries and keys of `tokens` normed and rotated (dc_qk_norm_rope).  With v the rotated
@@ -238,14 +239,14 @@ class DecodeBuffers:
         ld_q, ld_k = self._rows_of(q, hq, tokens, "q"), self._rows_of(k, hk, tokens, "k")
         if pos is not None:
             self._ints(pos, (tokens.tokens,), "pos")
-        q_out = self._empty(q.shape, q.dtype, stream) if q_out is None else self._like(q_out, tokens, hq, "q_out")
+        q_out = self._empty(q.shape, stream) if q_out is None else self._like(q_out, tokens, hq, "q_out")
         ld_v = 0
         if v is not None:
             if k_out is not None:
                 raise ValueError("with v the keys go to the cache: no k_out")
             ld_v = self._rows_of(v, hk, tokens, "v")
         else:
-            k_out = self._empty(k.shape, k.dtype, stream) if k_out is None else self._like(k_out, tokens, hk, "k_out")
+            k_out = self._empty(k.shape, stream) if k_out is None else self._like(k_out, tokens, hk, "k_out")
         B.dc_qk_norm_rope(self.dims, self.kv, layer, tokens, rope, q, ld_q, k, ld_k, v, ld_v, pos, q_out, k_out,
                           self._stream_here(stream))
         return q_out, k_out
@@ -254,14 +255,14 @@ class DecodeBuffers:
         need = B.dc_tokens_workspace_bytes(self.dims, tokens, self.kv.len + tokens.max_tokens)
         if need > self.ws_bytes:
             self._older_ws.append(self.ws)       # a captured graph may hold its address
-            self.ws = self._empty(need, torch.uint8, stream)
+            self.ws = self._empty(-(-need // self.k.element_size()), stream).view(torch.uint8)
             self.ws_bytes = need
 
     def _check_queries(self, tokens, q, out, stream):
         self._batch_of(tokens)
         hq = self.dims.n_q_heads
         self._like(q, tokens, hq, "q")
-        return self._empty(q.shape, q.dtype, stream) if out is None else self._like(out, tokens, hq, "out")
+        return self._empty(q.shape, stream) if out is None else self._like(out, tokens, hq, "out")
 
     def prompt_attention(self, tokens, q, layer=0, out=None, stream=None):
         """Causal attention of packed prompts whose K/V are behind the cache's rows."""

@@ -827,6 +827,8 @@ dc_status dc_kl_reward_static(int32_t rows, int32_t hidden, int32_t vocab, const
 
 namespace {
 
+constexpr int MAX_TOKENS = 1 << 25;     // of one call
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 dc_status check_tokens(const dc_dims* dims, const dc_tokens* t) {
@@ -834,6 +836,7 @@ dc_status check_tokens(const dc_dims* dims, const dc_tokens* t) {
   if (st != DC_OK) return st;
   if (!t) return DC_ERR_NULL;
   if (t->tokens < 1 || t->max_tokens < 1 || t->max_tokens > t->tokens) return DC_ERR_SHAPE;
+  if (t->tokens > MAX_TOKENS) return DC_ERR_UNSUPPORTED;
   const int64_t most = (int64_t)dims->batch * t->max_tokens;
   if (t->cu ? t->tokens > most : t->tokens != most) return DC_ERR_SHAPE;
   return DC_OK;

@@ -677,7 +677,8 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   a.splits = (int)splits;
   a.chunk = (int)chunk;
   a.ntiles = (int)nt;
-  return pairs * nt * splits < (1ll << 31) && pairs * ((rows + 3) / 4) < (1ll << 31);
+  // a launch counts its threads in 32 bits: 2^24 workgroups of 256
+  return pairs * nt * splits < (1 << 24) && (splits == 1 || pairs * ((rows + 3) / 4) < (1 << 24));
 }
 
 int launch_attend(const AttendArgs& a, int dtype, int D, void* stream) {

@@ -40,6 +40,7 @@ __device__ __forceinline__ uint4 pack_slice(const float* f) {
 // plain loads 138, three rows in flight 138 (fewer waves fit), tokens by two 157.
 constexpr int TPB = 4;               // (a wave each for their places)
 constexpr int FEW_WGS = 4096;
+static_assert(TPB * 64 <= RT, "a wave per token");
 
 template <int DTYPE, int D, int BATCH>
 __global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_block, int passes) {
@@ -202,7 +203,7 @@ template <int DTYPE, int D>
 __global__ void __launch_bounds__(RT) commit_path_kernel(CommitArgs a) {
   using R = RowT<DTYPE, D>;
   constexpr int LPR = R::LPR, RPP = RT / LPR;
-  const int u = a.y0 + blockIdx.x, b = u / a.per_seq;
+  const int u = a.y0 + blockIdx.y, b = u / a.per_seq;
   const int c = threadIdx.x % LPR, jr = threadIdx.x / LPR;
   int t0, n;
   token_range(a.tok, b, t0, n);
@@ -271,7 +272,11 @@ void norm_rope(const NormRopeArgs& a, hipStream_t s) {
 template <int DTYPE, int D>
 void commit(const CommitArgs& a, hipStream_t s) {
   if (a.path) {
-    hipLaunchKernelGGL((commit_path_kernel<DTYPE, D>), dim3(a.units), dim3(RT), 0, s, a);
+    for_grid_y(a.units, [&](int y0, int ny) {
+      CommitArgs b = a;
+      b.y0 = y0;
+      hipLaunchKernelGGL((commit_path_kernel<DTYPE, D>), dim3(1, ny), dim3(RT), 0, s, b);
+    });
     return;
   }
   if (a.alpha) {

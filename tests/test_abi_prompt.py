@@ -101,6 +101,15 @@ def test_attention_needs_its_workspace():
     assert B.dc_tokens_workspace_bytes(dims, tok, 0) == 0
 
 
+def test_sizes_past_the_grid_are_refused():
+    assert rope(dims=_dims(capacity=1 << 26), tok=_tok(1 << 26, 1 << 25)) == UNSUPPORTED
+    # 4096 sequences x 2 KV heads x 3125 tiles of 128 rows
+    big = _dims(batch=4096, capacity=1 << 20)
+    for tree in (False, True):
+        assert attend(tree, dims=big, tok=_tok(1 << 20, 100000, FAKE), ws=FAKE, wsb=1 << 60) == UNSUPPORTED
+    assert B.dc_tokens_workspace_bytes(big, _tok(1 << 20, 100000, FAKE), 1 << 20) == 0
+
+
 def test_workspace_for_longer_caches_covers_shorter_ones():
     for dtype in (B.DC_F32, B.DC_BF16):
         for batch, hk, n in ((1, 1, 1), (1, 8, 13), (2, 2, 300), (16, 8, 32)):

@@ -106,6 +106,11 @@ def close(got, want, keys, vmax, dtype):
     return np.all(np.abs(got - want) <= 2 * (H * np.abs(want) + off))
 
 
+def random_tree(n, seed):
+    g = np.random.default_rng(seed)
+    return [int(g.integers(-1, i)) if i else -1 for i in range(n)]
+
+
 def uneven(units, rows):
     return [max(0, rows - (5 * i) % 7 * (rows // 9)) for i in range(units)]
 
@@ -219,6 +224,77 @@ def test_prompt_attention(dtype, D, hk, G, counts, rows, lens):
     check_attention(c, out, layers - 1, [op.causal_mask(n) for n in counts])
 
 
+# Calls with enough workgroups for the tiles of 128 rows and of 64 (bf16, up to 64 rows of a
+# sequence and KV head), whole and in parts of the key range, as prompts and as trees.
+MANY = [([130, 0, 97, 40] * 3 + [33], 70, 8, 4, False), ([16, 3, 1, 9] * 5, 290, 8, 4, True),
+        ([300, 17], 900, 8, 8, False), ([60] * 9, 0, 8, 1, False)]
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("counts,rows,hk,G,lens", MANY)
+def test_many_rows(dtype, D, tree, counts, rows, hk, G, lens):
+    if tree and max(counts) > 256:
+        counts = [256, 17]
+    print(f"many rows {dtype} D={D} tree={tree} counts={counts[:4]}", flush=True)
+    c = Cache(counts, rows, dtype, D, hk, G, 1, uneven(len(counts) * hk, rows) if lens else None, seed=rows + D)
+    if tree:
+        parents = [random_tree(n, 5 * b + n) for b, n in enumerate(counts)]
+        flat = torch.tensor(sum(parents, []), dtype=torch.int32, device="cuda")
+        check_attention(c, c.buf.tree_attention(c.tokens, flat, c.q), 0, [op.tree_mask(p) for p in parents])
+    else:
+        check_attention(c, c.buf.prompt_attention(c.tokens, c.q), 0, [op.causal_mask(n) for n in counts])
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("counts,rows,hk,G,lens", MANY)
+def test_many_rows_do_not_depend_on_unseen_values(dtype, D, counts, rows, hk, G, lens):
+    c = Cache(counts, rows, dtype, D, hk, G, 1, uneven(len(counts) * hk, rows) if lens else None, seed=rows + D)
+    want = c.buf.prompt_attention(c.tokens, c.q)
+    at = [(b, t0, n // 2) for b, t0, n in c.spans() if n > 1]
+    for b, t0, r in at:
+        for h in range(hk):
+            u = c.unit(b, 0, h)
+            c.buf.v[u, c.lens[u] + r:] = float("inf") if h % 2 else float("nan")
+            c.buf.k[u, c.lens[u] + r:] = float("nan") if h % 2 else -float("inf")
+    got = c.buf.prompt_attention(c.tokens, c.q)
+    for b, t0, r in at:
+        assert close(got[t0:t0 + r], want[t0:t0 + r], rows + max(counts), 6, dtype), b
+        assert not torch.isfinite(got[t0 + r].float()).any()
+
+
+def test_a_query_that_is_not_a_number_stays_alone():
+    for dtype in ("bf16", "f32"):
+        c = Cache([50], 100, dtype, 128, 2, 4, seed=14)
+        want = c.buf.prompt_attention(c.tokens, c.q)
+        c.q[7, 3, 5] = float("nan")
+        c.q[9, 6] = float("inf")
+        got = c.buf.prompt_attention(c.tokens, c.q)
+        assert torch.isnan(got[7, 3]).all() and torch.isnan(got[9, 6]).all()
+        got[7, 3], got[9, 6] = want[7, 3], want[9, 6]
+        assert close(got, want, 150, 6, dtype)
+
+
+def test_a_scale_of_its_own():
+    c = Cache([21], 60, "bf16", 64, 2, 2, seed=15)
+    base = c.buf.prompt_attention(c.tokens, c.q)
+    c.buf.dims.scale = 0.25
+    got = c.buf.prompt_attention(c.tokens, c.q)
+    c.q = (c.q.float() * 2).to(c.td)                # 0.25 = 2 / sqrt(64): powers of two, exact
+    c.buf.dims.scale = 0.0
+    assert torch.equal(got, c.buf.prompt_attention(c.tokens, c.q)) and not torch.equal(got, base)
+
+
+def test_a_cache_past_the_memory_side_cache():
+    # over 256 MB of rows that are read once: other loads
+    c = Cache([5], 70000, "bf16", 128, 8, 4, seed=16)
+    check_attention(c, c.buf.prompt_attention(c.tokens, c.q), 0, [op.causal_mask(5)])
+    c = Cache([16], 70000, "f32", 64, 8, 4, seed=17)
+    p = random_tree(16, 3)
+    check_attention(c, c.buf.tree_attention(c.tokens, torch.tensor(p, dtype=torch.int32, device="cuda"), c.q), 0,
+                    [op.tree_mask(p)])
+
+
 def test_prompt_attention_does_not_depend_on_unseen_rows():
     # value and key rows that a token does not see: infinite, NaN and the largest numbers
     for dtype in ("bf16", "f32"):
@@ -295,11 +371,6 @@ def test_offsets_past_32_bits():
 
 
 # ------------------------------------------------------------------------ tree attention
-
-def random_tree(n, seed, deep=False):
-    g = np.random.default_rng(seed)
-    return [int(i - 1 if deep else g.integers(-1, i)) if i else -1 for i in range(n)]
-
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D,hk,G", [(128, 2, 4), (64, 1, 8), (64, 3, 1)])
