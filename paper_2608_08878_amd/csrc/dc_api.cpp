@@ -867,7 +867,8 @@ bool plan_attend(const dc_dims* dims, const dc_tokens* t, int L, dc::AttendArgs&
   a.cap = dims->capacity;
   a.scale = scale_of(dims);
   const bool ok = dc::attend_plan(a, dims->dtype, dims->head_dim, L);
-  need = a.splits > 1 ? align256((size_t)t->tokens * a.hq * a.splits * (dims->head_dim + 2) * sizeof(float)) : 0;
+  const size_t each = (size_t)t->tokens * a.hq * (dims->head_dim + 2) * sizeof(float);
+  need = a.most_splits > 1 ? align256(each * a.most_splits) : 0;
   return ok;
 }
 

@@ -687,12 +687,32 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   int bm = 128;
   if (rows <= 32 || tiles(128) * parts < CUS) bm = 32;
   else if (rows <= 64 && dtype == 1) bm = 64;
-  // parts for every workgroup that the CUs hold at a time
+  // Parts of the key range, at most as many as the CUs hold workgroups at a time.  More parts shorten
+  // a workgroup's walk over the keys and lengthen the join, whose outputs in float32 are written and
+  // read: the number with the least of both, from what was measured (us): a walk's step of `bn` keys
+  // 1.3 alone on a CU and 2 beside another (bf16, 128 elements), joined outputs at 3.5 TB/s.  One prompt
+  // of 512 tokens 21 -> 16 us against as many parts as fit, of 1024 37 -> 27; 256 behind 16384 rows
+  // 94, with half as many parts 102, in one 330.
   const int per_cu = bm == 128 || (dtype == 1 && D == 64) ? 2 : 1;
-  int64_t splits = per_cu * CUS / tiles(bm);
-  splits = splits > parts ? parts : splits;
-  splits = splits > MAX_PARTS ? MAX_PARTS : splits < 1 ? 1 : splits;
-  const int64_t chunk = ((L + splits - 1) / splits + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK;
+  int64_t most = per_cu * CUS / tiles(bm);
+  most = most > parts ? parts : most;
+  most = most > MAX_PARTS ? MAX_PARTS : most < 1 ? 1 : most;
+  const int bn = bm == 128 ? (dtype == 1 ? 64 : 32) : dtype == 1 || D == 64 ? 128 : 64;
+  const double step = dtype == 1 ? 0.5 + 0.8 * D / 128 : 3.6 * D / 128;
+  const double seen = 1.0 - 0.5 * a.tok.max_tokens / L;       // of the parts, by the average row
+  int64_t splits = 1, chunk = (L + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK;
+  double least = 0.0;
+  for (int64_t n = 1; n <= most; ++n) {
+    const int64_t c = ((L + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK, real = (L + c - 1) / c;
+    const double walk = (double)((c + bn - 1) / bn) * step * (per_cu == 2 && tiles(bm) * real > CUS ? 1.55 : 1.0);
+    const double join = n > 1 ? 3.0 + (double)a.tok.tokens * a.hq * real * seen * D * 8 / 3.5e6 : 0.0;
+    if (n == 1 || walk + join < least) {
+      least = walk + join;
+      splits = real;
+      chunk = c;
+    }
+  }
+  a.most_splits = (int)most;
   const int64_t nt = (rows + bm - 1) / bm;
   a.bm = bm;
   // Rows that one row tile reads, once, and that no cache holds anyway: non-temporal (16 x 32 drafted
@@ -702,7 +722,7 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   a.chunk = (int)chunk;
   a.ntiles = (int)nt;
   // a launch counts its threads in 32 bits: 2^24 workgroups of 256
-  return pairs * nt * splits < (1 << 24) && (splits == 1 || pairs * ((rows + 3) / 4) < (1 << 24));
+  return pairs * nt * most < (1 << 24) && (most == 1 || pairs * ((rows + 3) / 4) < (1 << 24));
 }
 
 int launch_attend(const AttendArgs& a, int dtype, int D, void* stream) {

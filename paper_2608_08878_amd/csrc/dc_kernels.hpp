@@ -187,6 +187,7 @@ struct AttendArgs {
   int batch, n_layers, layer, hq, hk, gshift, len;
   float scale;
   int splits;               // parts of the key range, `chunk` rows each
+  int most_splits;          // what the workspace is sized for: grows with the cache
   int chunk;
   int ntiles;               // row tiles of the longest sequence
   int bm;                   // rows of a tile
