@@ -348,9 +348,9 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, size_t qrow, int 
     }
 }
 
-// The same of the wave's 32 rows.  A lane holds pieces of 16 bytes of one row; they cross LDS (`st`, 128 D bytes of the wave's own, chunk c
-// of row r at c ^ r) so that the stores are whole rows
-// (16 prompts of up to 255 tokens 24.0 -> 20.6 us; a call of few rows, whose latency counts, is faster
+// The same of the wave's 32 rows.  A lane holds pieces of 16 bytes of one row; they cross LDS (`st`,
+// 128 D bytes of the wave's own, chunk c of row r at c ^ r) so that the stores are whole rows (16
+// prompts of up to 255 tokens 24.0 -> 20.6 us; a call of few rows, whose latency counts, is faster
 // without: 512 float32 tokens 12.2, with 12.9).
 template <int DT, int D>
 __device__ __forceinline__ void store_rows(const AttendArgs& a, const Place& w, int wrow, char* st, const f32x16_t* o,
@@ -396,6 +396,13 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const Place& w, 
   }
 }
 
+// Bound by the matrix cores and, at that, by power: two prompts of 8192 tokens (32/8 heads of 128) 1045 us =
+// 1.05 PFLOP/s at a clock of 1.8 GHz, where a large library product reaches 1.35; on zeros 860.  Two waves a
+// SIMD (256 registers each; one wave 1861) overlap one's softmax with the other's products.  Tried and not
+// kept: three key blocks in hand in a wave 1075-1086, 64 rows a wave 1455, eight waves a workgroup 1105, tiles
+// of 32 keys 1112.  With 64-element heads the exponentials bound it (4 x 2048 tokens, 64/8 heads: 180 us =
+// 0.76 PFLOP/s; tiles of 128 keys 209).  Few rows over long caches are bound by HBM: 160 drafted
+// tokens over 16 caches of up to 16384 rows, 834 MB, 171-178 us (its loads alone 149).
 template <int DT, int D, int RW, int KW, int SK, bool TREE>
 __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES)) attend_kernel(AttendArgs a) {
   using T = KVT<DT, D>;
@@ -483,9 +490,7 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
       float mx = NEG_INF;
       const bool masked = kb + SK > full;
 #pragma unroll
-      for (int x = 0; x < SK / 32; ++x) {
-        s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
-      }
+      for (int x = 0; x < SK / 32; ++x) s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
       if (masked) {
 #pragma unroll
         for (int x = 0; x < SK / 32; ++x) mask32(s[x], sees32<TREE>(w, anc, r, kb + 32 * x), h);
@@ -511,8 +516,11 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
         for (int i = 0; i < 16; ++i) s[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], c, -mc));
         Weights<DT> p;
         p.set(s[x], l);
-        if (CAREFUL && masked) values32_masked<DT, D>(vl + 32 * x * T::RB, s[x], sees32<TREE>(w, anc, r, kb + 32 * x), o, lane);
-        else values32<DT, D>(vl + 32 * x * T::RB, p, o, lane);
+        const char* vx = vl + 32 * x * T::RB;
+        if (CAREFUL && masked)
+          values32_masked<DT, D>(vx, s[x], sees32<TREE>(w, anc, r, kb + 32 * x), o, lane);
+        else
+          values32<DT, D>(vx, p, o, lane);
       }
     };
     if constexpr (CAREFUL) load_tile(0, 0);

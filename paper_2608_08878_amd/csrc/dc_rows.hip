@@ -33,13 +33,13 @@ __device__ __forceinline__ uint4 pack_slice(const float* f) {
 // A workgroup takes up to TPB tokens.  It first puts their angles and places in LDS, one
 // angle per thread, for every head; then LPR lanes work on a head row, 16 bytes each, the
 // half-split partner a lane exchange away, with BATCH rows' loads under way at a time.
-// One token and one row per lane group where that makes no more than FEW_WGS workgroups (a step's
-// 16 tokens 8.4 -> 6.3 us, 1557 float32 tokens 6.4 -> 5.3), else TPB tokens: a workgroup's angles and
-// places cost about 2 us of latency before its first store (16k tokens 437 us one at a time).
-// 20001 tokens of 32 + 16 heads of 128, 481 MB: 127 us = 3.8 TB/s, of the 4.8 that a copy reaches;
-// plain loads 138, three rows in flight 138 (fewer waves fit), tokens by two 157.
+// One token and one row per lane group where that makes no more than FEW_WGS workgroups, else TPB
+// tokens: a workgroup's angles and places are a chain of loads before its first store, which many
+// small ones repeat and few large ones show (32 + 16 heads of 128, one token at a time and by four:
+// 64 tokens 4.3 and 12.7 us, 1024 9.2 and 15.6, 4096 29.9 and 31.4, 20001 142 and 107).
+// 20001 tokens, 481 MB, 107 us = 4.5 TB/s, of the 4.8 that a copy reaches.
 constexpr int TPB = 4;               // (a wave each for their places)
-constexpr int FEW_WGS = 4096;
+constexpr int FEW_WGS = 16384;
 static_assert(TPB * 64 <= RT, "a wave per token");
 
 template <int DTYPE, int D, int BATCH>
@@ -47,6 +47,7 @@ __global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_b
   using R = RowT<DTYPE, D>;
   constexpr int LPR = R::LPR, EPL = R::EPL, ELT = R::ELT, GROUPS = RT / LPR;
   __shared__ __attribute__((aligned(16))) float cs[TPB][MAX_PAIRS], sn[TPB][MAX_PAIRS];
+  __shared__ __attribute__((aligned(16))) float gain[2 * D];
   __shared__ int seq[TPB], num[TPB];                  // a token's sequence and number there, or -1
   const int tid = threadIdx.x, c = tid % LPR, grp = tid / LPR;
   const int half = a.rot / 2, dist = half / EPL;      // half-split partner: dist lanes away
@@ -86,13 +87,19 @@ __global__ void __launch_bounds__(RT) norm_rope_kernel(NormRopeArgs a, int per_b
       num[x] = r >= 0 && r < n ? r : -1;
     }
   }
+  // gains through LDS: a load a thread (each lane its 16 of them straight into registers took
+  // 9 us more of 512 tokens' 15)
+  if (a.norm && tid < 2 * D) {
+    const float* from = tid < D ? a.q_gain : a.k_gain;
+    gain[tid] = from ? from[tid % D] : 1.0f;
+  }
+  __syncthreads();
   float gq[EPL], gk[EPL];
 #pragma unroll
   for (int e = 0; e < EPL; ++e) {
-    gq[e] = a.q_gain ? a.q_gain[c * EPL + e] : 1.0f;
-    gk[e] = a.k_gain ? a.k_gain[c * EPL + e] : 1.0f;
+    gq[e] = gain[c * EPL + e];
+    gk[e] = gain[D + c * EPL + e];
   }
-  __syncthreads();
 
   auto finish = [&](int i, uint4 x16) {
     const int t = i / passes, row = row0 + (i - t * passes) * GROUPS + grp;

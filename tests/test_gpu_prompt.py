@@ -179,10 +179,13 @@ def test_norm_rope(dtype, D, rot, inter, norm, far):
             rope_case(c, layers - 1, rot, inter, norm, far, cache, gains=inter or far > 90)
 
 
-def test_norm_rope_of_many_tokens():
-    # over the size at which a workgroup takes several tokens
-    c = Cache([4001, 0, 4095, 200], 0, "bf16", 64, 1, 2, seed=5, lens=[0] * 4)
-    rope_case(c, 0, 64, False, True, 9000, True)
+@pytest.mark.parametrize("counts,dtype,D,hk,G", [([8001, 0, 8195, 300], "bf16", 64, 1, 2),
+                                                 ([1700, 1306], "f32", 128, 8, 4)])
+def test_norm_rope_of_many_tokens(counts, dtype, D, hk, G):
+    # over the size from which a workgroup takes several tokens
+    c = Cache(counts, 0, dtype, D, hk, G, seed=5, lens=[0] * (len(counts) * hk))
+    rope_case(c, 0, D, False, True, 9000, True)
+    rope_case(c, 0, D // 2, True, True, 9000, False)
 
 
 def test_norm_rope_in_place_and_single_heads():
