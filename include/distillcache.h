@@ -581,6 +581,7 @@ size_t dc_tokens_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, i
  * K and V of the path move in place.  Afterwards unit_len[u] += rows kept, kv->len +=
  * width, feat->next_pos += width (host: the caller may lower kv->len to any bound of the
  * unit lengths that it knows, and next_pos to any value past the positions in use).
+ * A unit may stay at 0 rows (an empty prompt of a batch); a decode step takes at least one.
  * Equal counts need nothing else; cu or keep make the units' lengths differ, which
  * takes a ragged cache.
  * Errors: DC_ERR_NULL (dims, kv, tokens, buffers; cu or keep without kv->unit_len),

@@ -109,7 +109,8 @@ __device__ __forceinline__ f32x16_t scores32(const char* k, const uint4* qf, int
 // The weights of 32 keys as the matrix cores take them; p[i] is that of key key_of(i, h).  bf16: each
 // is rounded by up to half a step, 2^-8 of itself.  Their sum is taken of the rounded ones, so that
 // the output is a mean by the weights that were used: where one key has nearly all weight its rounding
-// cancels (relative error of the outputs, 8192 keys: 0.0019 with the sum of the unrounded ones).
+// cancels (relative error of the outputs, two prompts of 8192 tokens: 0.0017, with the sum of the unrounded
+// ones 0.0019).
 template <int DT>
 struct Weights {
   f32x16_t f;
@@ -692,9 +693,18 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
     return all < nt * pairs ? all : nt * pairs;
   };
   const int64_t parts = (L + MIN_CHUNK - 1) / MIN_CHUNK;
+  const int64_t bytes = pairs * L * 2 * D * (dtype == 1 ? 2 : 4);      // of K and V
+  // Rows of a tile.  32, the keys cut among the waves, for up to 32 rows and where tiles of 128 would
+  // leave CUs idle (measured against 128: 512 float32 tokens of 4/2 heads of 64 11.7 and 17.7 us, 256
+  // tokens of 32/8 heads 9.3 and 10.5, one token of 8 sequences in float32 109 and 190; past that point
+  // 128 rows are faster, 512 tokens 16.2 and with 32 18.4).  64 and two groups of keys for up to 64 bf16
+  // rows (13 tokens behind 4096 13.5 us, with 128 rows 14.8).  Both hold a CU's LDS alone with heads of
+  // 128 elements, and caches that only HBM holds stream faster by two workgroups: there 128 rows (one
+  // token of 16 sequences of 4096 rows 49 us, with 32 rows 56; 16 tokens, 16384 rows, 188, with 64 206).
+  const bool stream = dtype == 1 && D == 128 && bytes > BIG_CACHE / 4 * 3;
   int bm = 128;
-  if (rows <= 32 || tiles(128) * parts < CUS) bm = 32;
-  else if (rows <= 64 && dtype == 1) bm = 64;
+  if (!stream && (rows <= 32 || tiles(128) * parts < CUS)) bm = 32;
+  else if (!stream && rows <= 64 && dtype == 1) bm = 64;
   // Parts of the key range, at most as many as the CUs hold workgroups at a time.  More parts shorten
   // a workgroup's walk over the keys and lengthen the join, whose outputs in float32 are written and
   // read: the number with the least of both, from what was measured (us): a walk's step of `bn` keys
@@ -725,7 +735,7 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   a.bm = bm;
   // Rows that one row tile reads, once, and that no cache holds anyway: non-temporal (16 x 32 drafted
   // tokens over 16k rows, 834 MB, 191 -> 180 us; 13 over 4k rows, 17 MB, 15.6 -> 16.8)
-  a.once = nt == 1 && pairs * L * 2 * D * (dtype == 1 ? 2 : 4) > BIG_CACHE;
+  a.once = nt == 1 && bytes > BIG_CACHE;
   a.splits = (int)splits;
   a.chunk = (int)chunk;
   a.ntiles = (int)nt;
