@@ -210,6 +210,15 @@ class DecodeBuffers:
         n = getattr(tokens, "sequences", self.dims.batch)
         if n != self.dims.batch:
             raise ValueError(f"tokens of {n} sequences for a cache of {self.dims.batch}")
+        if getattr(tokens, "device", self._device) != self._device:
+            raise ValueError(f"the tokens' offsets are on cuda:{tokens.device}, the cache on {self.k.device}")
+
+    def _rope_of(self, rope):
+        """What make_rope noted of its vectors, against this cache."""
+        if getattr(rope, "gain_len", self.D) != self.D:
+            raise ValueError(f"gains of {rope.gain_len} elements for heads of {self.D}")
+        if getattr(rope, "device", self._device) != self._device:
+            raise ValueError(f"the rotation's vectors are on cuda:{rope.device}, the cache on {self.k.device}")
 
     def _here(self, x, name):
         if x.get_device() != self._device:
@@ -236,6 +245,7 @@ class DecodeBuffers:
         returned too.  Returns (q_out, k_out or None)."""
         hq, hk = self.dims.n_q_heads, self.dims.n_kv_heads
         self._batch_of(tokens)
+        self._rope_of(rope)
         ld_q, ld_k = self._rows_of(q, hq, tokens, "q"), self._rows_of(k, hk, tokens, "k")
         if pos is not None:
             self._ints(pos, (tokens.tokens,), "pos")
@@ -309,6 +319,10 @@ class DecodeBuffers:
 def make_tokens(counts, device="cuda") -> B.dc_tokens:
     """Packed tokens of sequences of `counts` (host) tokens each."""
     counts = [int(c) for c in counts]
+    if torch.device(device).type != "cuda":
+        raise ValueError(f"the tokens' offsets must be on a GPU, got {device}")
+    if not counts or min(counts) < 0 or sum(counts) >= 1 << 31:
+        raise ValueError("counts must be one or more numbers of tokens, at least 0, their sum below 2^31")
     most, total = max(counts), sum(counts)
     t = B.dc_tokens(total, most, None)
     t.sequences = len(counts)
@@ -318,17 +332,30 @@ def make_tokens(counts, device="cuda") -> B.dc_tokens:
             cu.append(cu[-1] + c)
         t.cu_tensor = torch.tensor(cu, dtype=torch.int32, device=device)   # kept alive with t
         t.cu = t.cu_tensor.data_ptr()
+        t.device = t.cu_tensor.get_device()
     return t
 
 
 def make_rope(inv_freq=None, interleaved=False, norm=False, eps=1e-6, q_gain=None, k_gain=None) -> B.dc_rope:
-    """Norm and rotation of a head; inv_freq [rot_dim / 2] float32 on the device (None: no rotation)."""
-    for name, x in (("inv_freq", inv_freq), ("q_gain", q_gain), ("k_gain", k_gain)):
-        if x is not None and (x.dtype != torch.float32 or x.dim() != 1 or not x.is_contiguous()):
+    """Norm and rotation of a head; inv_freq [rot_dim / 2] float32 (None: no rotation), gains
+    [head_dim] float32, all on the cache's device."""
+    given = [(name, x) for name, x in (("inv_freq", inv_freq), ("q_gain", q_gain), ("k_gain", k_gain))
+             if x is not None]
+    for name, x in given:
+        if x.dtype != torch.float32 or x.dim() != 1 or not x.is_contiguous():
             raise ValueError(f"{name} must be a contiguous float32 vector")
+        if not x.is_cuda or x.device != given[0][1].device:
+            raise ValueError(f"{name} is on {x.device}: all must be on the cache's GPU")
+    if q_gain is not None and k_gain is not None and q_gain.numel() != k_gain.numel():
+        raise ValueError(f"gains of {q_gain.numel()} and {k_gain.numel()} elements")
     r = B.dc_rope(int(norm), eps, B._ptr(q_gain), B._ptr(k_gain),
                   0 if inv_freq is None else 2 * inv_freq.numel(), int(interleaved), B._ptr(inv_freq))
     r.tensors = (inv_freq, q_gain, k_gain)       # kept alive with r
+    if given:
+        r.device = given[0][1].get_device()
+    gain = q_gain if q_gain is not None else k_gain
+    if gain is not None:
+        r.gain_len = gain.numel()
     return r
 
 
