@@ -107,11 +107,21 @@ class DecodeBuffers:
         torch.cuda.synchronize(dev)
 
     def reserve_workspace(self, max_len: int, kl_rows: int = 0, kl_vocab: int = 0):
-        need = B.dc_workspace_bytes(self.dims, max_len, kl_rows, kl_vocab)
-        if need > self.ws_bytes:
-            self.ws = torch.empty(need, dtype=torch.uint8, device=self.k.device)
-            self.ws_bytes = need
+        self._grow(B.dc_workspace_bytes(self.dims, max_len, kl_rows, kl_vocab))
         return self.ws
+
+    def _grow(self, need: int, stream=None):
+        """A workspace of at least `need` bytes.  A captured graph may hold an outgrown one's
+        address, so those live as long as the buffers; each is at least twice the one before,
+        so that they add up to less than the present one."""
+        if need <= self.ws_bytes:
+            return
+        if self.ws is not None:
+            self._older_ws.append(self.ws)
+            need = max(need, 2 * self.ws_bytes)
+        need = -(-need // 16) * 16
+        self.ws = self._empty((need // self.k.element_size(),), stream).view(torch.uint8)
+        self.ws_bytes = need
 
     def feat_init(self, length: int, first_pos: int = 0, stream=None):
         self.kv.len = length
@@ -261,12 +271,12 @@ class DecodeBuffers:
                           self._stream_here(stream))
         return q_out, k_out
 
-    def _tokens_workspace(self, tokens, stream):
-        need = B.dc_tokens_workspace_bytes(self.dims, tokens, self.kv.len + tokens.max_tokens)
-        if need > self.ws_bytes:
-            self._older_ws.append(self.ws)       # a captured graph may hold its address
-            self.ws = self._empty(-(-need // self.k.element_size()), stream).view(torch.uint8)
-            self.ws_bytes = need
+    def reserve_tokens_workspace(self, tokens, max_len: int, stream=None):
+        """Scratch of the attention of such tokens over caches of up to max_len rows, the tokens' own
+        included.  The calls reserve what they need themselves; reserved once for the longest cache,
+        it does not grow on the way.  All calls of one DecodeBuffers share it: they, and replays of
+        graphs that captured them, run one after the other."""
+        self._grow(B.dc_tokens_workspace_bytes(self.dims, tokens, max_len), stream)
 
     def _check_queries(self, tokens, q, out, stream):
         self._batch_of(tokens)
@@ -277,7 +287,7 @@ class DecodeBuffers:
     def prompt_attention(self, tokens, q, layer=0, out=None, stream=None):
         """Causal attention of packed prompts whose K/V are behind the cache's rows."""
         out = self._check_queries(tokens, q, out, stream)
-        self._tokens_workspace(tokens, stream)
+        self.reserve_tokens_workspace(tokens, self.kv.len + tokens.max_tokens, stream)
         B.dc_prompt_attention(self.dims, self.kv, layer, tokens, q, out, self.ws, self.ws_bytes,
                               self._stream_here(stream))
         return out
@@ -286,7 +296,7 @@ class DecodeBuffers:
         """Attention of drafted tokens over the cache, themselves and their ancestors."""
         out = self._check_queries(tokens, q, out, stream)
         self._ints(parent, (tokens.tokens,), "parent")
-        self._tokens_workspace(tokens, stream)
+        self.reserve_tokens_workspace(tokens, self.kv.len + tokens.max_tokens, stream)
         B.dc_tree_attention(self.dims, self.kv, layer, tokens, parent, q, out, self.ws, self.ws_bytes,
                             self._stream_here(stream))
         return out
