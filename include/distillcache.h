@@ -64,6 +64,7 @@ typedef enum {
 typedef enum { DC_F32 = 0, DC_BF16 = 1 } dc_dtype;
 
 #define DC_MAX_WINDOW 64
+#define DC_BEHIND_ROWS (DC_MAX_WINDOW + 2)
 
 /* Shapes.  Supported: head_dim in {64, 128}; G = n_q_heads / n_kv_heads in
  * {1, 2, 4, 8}; dtype DC_F32 or DC_BF16. */
@@ -119,7 +120,9 @@ typedef struct {
   float   *qstat;      /* [units][w][G][3]: (m, 1/l, H) of each query, where
                           m = max_i s_i, l = sum_i exp(s_i - m), s_i = scale * q.k_i */
   int32_t step;        /* host: decode steps done since the state was initialised */
-  int32_t next_pos;    /* host: T, the position the next appended token receives */
+  int32_t next_pos;    /* host: T, the position the next appended token receives.  It stays above
+                          every position in use and every ring_pmax of the last w steps.  (With
+                          `behind`: of a sequence that has seen every token of the batch) */
   int32_t ring_pmax[DC_MAX_WINDOW]; /* host: per ring slot, largest position present (T - 1) */
   float   *sigma;      /* [units][capacity] sigma_i of the last step, or NULL; written by
                           every decode step and dc_feat_init (0) when present, moved by
@@ -127,6 +130,16 @@ typedef struct {
   int32_t alpha_recent; /* 0: alpha accumulates over steps (cumulative attention);
                           1: every decode step replaces alpha by that step's mass (the
                           paper's "most recent forward pass"; see dc_global_alpha) */
+  int32_t *behind;     /* device [DC_BEHIND_ROWS][units] or NULL, contents the library's: what
+                          batches need whose sequences see different numbers of tokens
+                          (dc_commit_rows with cu or keep, ragged caches).  Row behind_row - 1
+                          holds by how many tokens every unit's sequence is behind next_pos:
+                          its own T, the position of its next token and the T of its pos / T
+                          are next_pos less that.  NULL, and row 0: all are at next_pos. */
+  int32_t behind_row;  /* host: the row in force, 0 for none.  Setting next_pos by hand puts
+                          every sequence at that T (row 0) */
+  int32_t behind_at;   /* host: the next_pos that behind_row belongs to */
+  int32_t ring_row[DC_MAX_WINDOW];  /* host: per ring slot, the row in force at that step */
 } dc_feat;
 
 /* Policy MLP f_phi (Sec. 3.1.2; a small ReLU MLP per App. D).  params is a
@@ -160,7 +173,7 @@ size_t dc_workspace_bytes(const dc_dims *dims, int32_t max_len, int32_t kl_rows,
 /* Initialise the feature state of a cache holding kv->len rows per unit whose
  * slot i holds the token at position first_pos + i (a freshly filled cache):
  * alpha = ent_num = ent_den = 0, pos, vnorm from the value rows; host fields
- * step = 0, next_pos = first_pos + kv->len. */
+ * step = 0, next_pos = first_pos + kv->len (of every sequence: behind_row = 0). */
 dc_status dc_feat_init(const dc_dims *dims, const dc_kv *kv, dc_feat *feat, int32_t first_pos,
                        void *hip_stream);
 
@@ -576,15 +589,18 @@ size_t dc_tokens_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, i
  *   keep   device [batch] int32 or NULL: rows that sequence b keeps, clamped to
  *          [0, min(width, its tokens)]; NULL: all of them.
  *   feat   NULL (a teacher cache) or the feature state, which gets the rows as
- *          dc_feat_init would: alpha = ent_num = ent_den = sigma = 0, vnorm, and positions
- *          next_pos + j.
+ *          dc_feat_init would: alpha = ent_num = ent_den = sigma = 0, vnorm, and the
+ *          sequence's next positions, T + j.  cu and keep let the sequences' T differ, which
+ *          takes feat->behind.
  * K and V of the path move in place.  Afterwards unit_len[u] += rows kept, kv->len +=
- * width, feat->next_pos += width (host: the caller may lower kv->len to any bound of the
- * unit lengths that it knows, and next_pos to any value past the positions in use).
- * A unit may stay at 0 rows (an empty prompt of a batch); a decode step takes at least one.
+ * width, feat->next_pos += width, and a sequence's T by the rows that it keeps (host: the
+ * caller may lower kv->len to any bound of the unit lengths that it knows).
+ * A unit may stay at 0 rows (an empty prompt of a batch): the next step's append is its first
+ * row; a step without an append takes at least one.
  * Equal counts need nothing else; cu or keep make the units' lengths differ, which
  * takes a ragged cache.
- * Errors: DC_ERR_NULL (dims, kv, tokens, buffers; cu or keep without kv->unit_len),
+ * Errors: DC_ERR_NULL (dims, kv, tokens, buffers; cu or keep without kv->unit_len, or with
+ * feat and without feat->behind),
  * DC_ERR_SHAPE, DC_ERR_CAPACITY (kv->len + max_tokens > capacity), DC_ERR_UNSUPPORTED. */
 dc_status dc_commit_rows(const dc_dims *dims, dc_kv *kv, dc_feat *feat, const dc_tokens *tokens,
                          const int32_t *path, const int32_t *keep, int32_t width, void *hip_stream);

@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdistillcache.so")
 
 MAX_WINDOW = 64
+BEHIND_ROWS = MAX_WINDOW + 2
 DC_F32, DC_BF16 = 0, 1
 STATUS = {0: "DC_OK", 1: "DC_ERR_NULL", 2: "DC_ERR_SHAPE", 3: "DC_ERR_UNSUPPORTED",
           4: "DC_ERR_CAPACITY", 5: "DC_ERR_BUDGET", 6: "DC_ERR_WORKSPACE", 7: "DC_ERR_HIP",
@@ -35,7 +36,9 @@ class dc_feat(ctypes.Structure):
                 ("vnorm", ctypes.c_void_p), ("qring", ctypes.c_void_p),
                 ("qstat", ctypes.c_void_p), ("step", ctypes.c_int32),
                 ("next_pos", ctypes.c_int32), ("ring_pmax", ctypes.c_int32 * MAX_WINDOW),
-                ("sigma", ctypes.c_void_p), ("alpha_recent", ctypes.c_int32)]
+                ("sigma", ctypes.c_void_p), ("alpha_recent", ctypes.c_int32),
+                ("behind", ctypes.c_void_p), ("behind_row", ctypes.c_int32), ("behind_at", ctypes.c_int32),
+                ("ring_row", ctypes.c_int32 * MAX_WINDOW)]
 
 
 class dc_policy(ctypes.Structure):

@@ -62,6 +62,10 @@ class DecodeBuffers:
                 # the fifth feature (needed by five-input policies)
                 self.sigma = torch.zeros((self.U, capacity), dtype=torch.float32, device=device)
                 self.feat.sigma = self.sigma.data_ptr()
+            if ragged:
+                # sequences that see different numbers of tokens
+                self.behind = torch.zeros((B.BEHIND_ROWS, self.U), dtype=torch.int32, device=device)
+                self.feat.behind = self.behind.data_ptr()
         self.ws = None
         self.ws_bytes = 0
         self._older_ws = []

@@ -31,6 +31,25 @@ dc_status check_dims(const dc_dims* d) {
   return DC_OK;
 }
 
+// Sequences of different counts (dc_feat.behind): row r of the table, 1 .. DC_BEHIND_ROWS, null for 0.
+dc_status check_behind(const dc_feat* f, const dc_kv* kv) {
+  if (!f || !f->behind) return DC_OK;
+  if (!kv->unit_len) return DC_ERR_NULL;
+  bool in = f->behind_row >= 0 && f->behind_row <= DC_BEHIND_ROWS;
+  for (int s = 0; s < DC_MAX_WINDOW; ++s) in = in && f->ring_row[s] >= 0 && f->ring_row[s] <= DC_BEHIND_ROWS;
+  return in ? DC_OK : DC_ERR_SHAPE;
+}
+int32_t* behind_at(const dc_dims* d, const dc_feat* f, int r) {
+  return f->behind && r > 0 ? f->behind + (size_t)(r - 1) * units_of(d) : nullptr;
+}
+// The row in force: none where the caller has set next_pos since.
+int behind_now(const dc_feat* f) { return f->behind && f->behind_at == f->next_pos ? f->behind_row : 0; }
+void advance_pos(dc_feat* f, int n, int row) {
+  f->next_pos += n;
+  f->behind_row = row;
+  f->behind_at = f->next_pos;
+}
+
 float scale_of(const dc_dims* d) { return d->scale > 0.0f ? d->scale : 1.0f / sqrtf((float)d->head_dim); }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -192,8 +211,10 @@ dc_status dc_feat_init(const dc_dims* dims, const dc_kv* kv, dc_feat* feat, int3
       return DC_ERR_HIP;
   }
   feat->step = 0;
-  feat->next_pos = first_pos + kv->len;
+  feat->next_pos = first_pos;
+  advance_pos(feat, kv->len, 0);
   memset(feat->ring_pmax, 0, sizeof(feat->ring_pmax));
+  memset(feat->ring_row, 0, sizeof(feat->ring_row));
   return DC_OK;
 }
 
@@ -250,6 +271,8 @@ dc_status prep_decode(const dc_dims* dims, const dc_kv* kv, const dc_feat* feat,
     if (W > 0 && (!feat->qring || !feat->qstat)) return DC_ERR_NULL;
     if (feat->step < 0 || feat->next_pos < 0) return DC_ERR_SHAPE;
     if (feat->alpha_recent != 0 && feat->alpha_recent != 1) return DC_ERR_VALUE;
+    st = check_behind(feat, kv);
+    if (st != DC_OK) return st;
   }
   const int len = kv->len;
   const int append = k_new != nullptr;
@@ -299,12 +322,14 @@ dc_status prep_decode(const dc_dims* dims, const dc_kv* kv, const dc_feat* feat,
     a.qring = feat->qring;
     a.qstat = feat->qstat;
     a.T = feat->next_pos + append;
+    a.behind = behind_at(dims, feat, behind_now(feat));
     a.arec = feat->alpha_recent;
     a.window = W;
     if (W > 0) {
       a.slot = feat->step % W;
       a.retire = feat->step >= W;
       a.pmax_ret = a.retire ? feat->ring_pmax[a.slot] : 0;
+      if (a.retire) a.behind_ret = behind_at(dims, feat, feat->ring_row[a.slot]);
     }
   }
   if (unit_scratch) {
@@ -339,8 +364,11 @@ dc_status launch_decode_any(const dc_dims* dims, const dc::DecodeArgs& a, bool f
 void commit_decode(dc_kv* kv, dc_feat* feat, const dc::DecodeArgs& a, int W) {
   kv->len = a.L;
   if (feat) {
-    feat->next_pos += a.append;
-    if (W > 0) feat->ring_pmax[a.slot] = feat->next_pos - 1;
+    advance_pos(feat, a.append, behind_now(feat));
+    if (W > 0) {
+      feat->ring_pmax[a.slot] = feat->next_pos - 1;
+      feat->ring_row[a.slot] = feat->behind_row;
+    }
     feat->step += 1;
   }
 }
@@ -369,6 +397,8 @@ dc_status prep_evict(const dc_dims* dims, const dc_kv* kv, const dc_feat* feat,
   if (L < 1 || L > dims->capacity) return DC_ERR_SHAPE;
   if (L > dc::evict_max_len()) return DC_ERR_UNSUPPORTED;
   if (T < 1) return DC_ERR_SHAPE;
+  st = check_behind(feat, kv);
+  if (st != DC_OK) return st;
   const int evict = budget < L;
   const bool ragged = kv->unit_len != nullptr;
   if (ragged && dims->dtype != DC_BF16) return DC_ERR_UNSUPPORTED;
@@ -398,6 +428,7 @@ dc_status prep_evict(const dc_dims* dims, const dc_kv* kv, const dc_feat* feat,
   e.ld_kept = e.budget;
   e.unit_len = kv->unit_len;
   e.T = T;
+  e.behind = behind_at(dims, feat, behind_now(feat));
   e.nh = policy->n_hidden_layers;
   e.h1 = policy->hidden[0];
   e.h2 = policy->n_hidden_layers == 2 ? policy->hidden[1] : 0;
@@ -995,12 +1026,16 @@ dc_status dc_commit_rows(const dc_dims* dims, dc_kv* kv, dc_feat* feat, const dc
   if (feat) {
     if (!feat->alpha || !feat->ent_num || !feat->ent_den || !feat->pos || !feat->vnorm) return DC_ERR_NULL;
     if (feat->next_pos < 0 || feat->next_pos > INT32_MAX - tokens->max_tokens) return DC_ERR_SHAPE;
+    st = check_behind(feat, kv);
+    if (st != DC_OK) return st;
   }
-  if ((tokens->cu || keep) && !kv->unit_len) return DC_ERR_NULL;
+  const bool uneven = tokens->cu || keep;
+  if (uneven && (!kv->unit_len || (feat && !feat->behind))) return DC_ERR_NULL;
   if (width < 1 || width > tokens->max_tokens) return DC_ERR_SHAPE;
   if (path && tokens->max_tokens > DC_TREE_MAX_NODES) return DC_ERR_UNSUPPORTED;
   dc::CommitArgs a;
   memset(&a, 0, sizeof(a));
+  int row = 0;
   a.k = kv->k;
   a.v = kv->v;
   if (feat) {
@@ -1011,6 +1046,17 @@ dc_status dc_commit_rows(const dc_dims* dims, dc_kv* kv, dc_feat* feat, const dc
     a.vnorm = feat->vnorm;
     a.sigma = feat->sigma;
     a.next_pos = feat->next_pos;
+    row = behind_now(feat);
+    a.behind = behind_at(dims, feat, row);
+    if (uneven) {
+      // a row of the table that neither the present nor a step of the window refers to
+      bool used[DC_BEHIND_ROWS + 1] = {};
+      used[row] = true;
+      for (int s = 0; s < DC_MAX_WINDOW; ++s) used[feat->ring_row[s]] = true;
+      row = 1;
+      while (used[row]) ++row;
+      a.behind_next = behind_at(dims, feat, row);
+    }
   }
   a.unit_len = kv->unit_len;
   a.path = path;
@@ -1023,7 +1069,7 @@ dc_status dc_commit_rows(const dc_dims* dims, dc_kv* kv, dc_feat* feat, const dc
   a.width = width;
   if (dc::launch_commit(a, dims->dtype, dims->head_dim, hip_stream) != 0) return DC_ERR_HIP;
   kv->len += width;
-  if (feat) feat->next_pos += width;
+  if (feat) advance_pos(feat, width, row);
   return DC_OK;
 }
 

@@ -196,6 +196,19 @@ __device__ __forceinline__ int rows_before(const int32_t* unit_len, int len, int
   return x < 0 ? 0 : x > len ? len : x;
 }
 
+// Tokens that unit u's sequence has seen (a sequence of an uneven batch: behind[u] fewer than
+// the batch's count), at least 1.
+template <typename Args>
+__device__ __forceinline__ int tokens_of(const Args& a, int u) {
+  if (!a.behind) return a.T;
+  const int t = a.T - __builtin_amdgcn_readfirstlane(a.behind[u]);
+  return t < 1 ? 1 : t;
+}
+// Largest position of unit u at the step that leaves the window.
+__device__ __forceinline__ int retired_pmax(const DecodeArgs& a, int u) {
+  return a.behind_ret ? a.pmax_ret - __builtin_amdgcn_readfirstlane(a.behind_ret[u]) : a.pmax_ret;
+}
+
 __device__ __forceinline__ void compiler_fence() { asm volatile("" ::: "memory"); }
 
 // 16 bytes per lane from global memory to LDS byte lds + 16 lane (lds uniform).

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(NT, 4) score_select_kernel(EvictArgs a) {
 __global__ void __launch_bounds__(256) score_kernel(EvictArgs a, uint64_t* keys, int kstride) {
   const int u = a.y0 + blockIdx.y;
   const size_t ub = (size_t)u * a.cap;
-  const float invT = 1.0f / (float)a.T;
+  const float invT = 1.0f / (float)tokens_of(a, u);
   const int L = unit_rows(a, u);
   if (L <= a.fused_rows) return;                         // served by the single-launch step
   if (!a.scores_out && unit_budget(a, u) >= L) return;   // a unit that keeps every row reads no key
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(256) score_kernel(EvictArgs a, uint64_t* keys,
 __global__ void __launch_bounds__(256) score_ext_kernel(EvictArgs a, uint64_t* keys, int kstride) {
   const int u = a.y0 + blockIdx.y;
   const size_t ub = (size_t)u * a.cap;
-  const float invT = 1.0f / (float)a.T;
+  const float invT = 1.0f / (float)tokens_of(a, u);
   const int L = unit_rows(a, u);
   if (L <= a.fused_rows) return;                         // served by the single-launch step
   if (!a.scores_out && unit_budget(a, u) >= L) return;   // a unit that keeps every row reads no key

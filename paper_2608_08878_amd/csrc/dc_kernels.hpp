@@ -30,6 +30,8 @@ struct DecodeArgs {
   int append;
   float scale;
   int T;                // tokens seen after the append
+  const int32_t* behind;      // [units] tokens fewer that a unit's sequence has seen, or null (see tokens_of)
+  const int32_t* behind_ret;  // the same at the step that leaves the window, or null
   int window;           // w (0 = unbounded)
   int slot;             // ring slot written by this step
   int retire;           // the step leaving the window has a ring record
@@ -71,6 +73,7 @@ struct EvictArgs {
   int L;
   int budget;           // kept rows after the call (min(budget, L))
   int T;
+  const int32_t* behind;  // [units] tokens fewer that a unit's sequence has seen, or null
   int nh;               // hidden layers (1 or 2)
   int h1, h2;
   int n_in;             // 4 or 5 policy inputs
@@ -209,6 +212,8 @@ struct CommitArgs {
   const int32_t* keep;      // [batch] or null
   int64_t cap;
   TokenArgs tok;
+  const int32_t* behind;    // [units] tokens fewer that a unit's sequence has seen, or null
+  int32_t* behind_next;     // the same with this call's, or null where it changes none
   int units, per_seq;       // per_seq = units of one sequence
   int len, width, next_pos;
   int y0;                   // first grid row of the launch (see for_grid_y)

@@ -204,7 +204,7 @@ score_mlp2_kernel(EvictArgs a, uint64_t* keys, int kstride) {
   const int h1 = a.h1, h2 = a.h2;
   const int L = unit_rows(a, u);   // this unit's rows (scores_out keeps stride a.L)
   const size_t ub = (size_t)u * a.cap;
-  const float invT = 1.0f / (float)a.T;
+  const float invT = 1.0f / (float)tokens_of(a, u);
   const float bout = const_params(a.params)[h1 * a.n_in + h1 + h2 * h1 + h2 + h2];
   // features of this lane's A row (the four lanes of a row load the same row);
   // the next row block's are requested while the current one is computed
@@ -570,7 +570,7 @@ score_ln2_kernel(EvictArgs a, uint64_t* keys, int kstride, int nq) {
   // the moments multiply by 1 / width and the scale uses the hardware
   // reciprocal square root (one rounding more each than a division)
   const float ih1 = 1.0f / (float)h1, ih2 = 1.0f / (float)h2;
-  const float invT = 1.0f / (float)a.T;
+  const float invT0 = 1.0f / (float)a.T;
   const float bout = const_params(a.params)[h1 * a.n_in + 3 * h1 + h2 * h1 + 3 * h2 + h2];
   const float cinv = sm[Y::O_C];
   char* xw = reinterpret_cast<char*>(sm) + Y::O_X + wave * 64 * 64;   // this wave's input slots
@@ -585,6 +585,7 @@ score_ln2_kernel(EvictArgs a, uint64_t* keys, int kstride, int nq) {
     // (a unit that keeps every row reads no key)
     if (rb >= L || L <= a.fused_rows || (!a.scores_out && unit_budget(a, u) >= L)) continue;
     const size_t ub = (size_t)u * a.cap;
+    const float invT = a.behind ? 1.0f / (float)tokens_of(a, u) : invT0;
     // the item's inputs, a lane per row: all 32 part slots to LDS
     Feat f;
     fetch_row(a, ub, rb + lane, L, f);

@@ -180,10 +180,18 @@ __device__ __forceinline__ int rows_kept(const CommitArgs& a, int b, int n) {
   return m;
 }
 
-// Feature state of a row as dc_feat_init leaves it (lane c of the row's LPR).
+// Tokens fewer than the batch's count that unit u's sequence had seen, and has once it keeps `keep`
+// rows of a call that counts for a.width.
+__device__ __forceinline__ int behind_of(const CommitArgs& a, int u) { return a.behind ? a.behind[u] : 0; }
+__device__ __forceinline__ void store_behind(const CommitArgs& a, int u, int keep) {
+  if (a.behind_next) a.behind_next[u] = behind_of(a, u) + a.width - keep;
+}
+
+// Feature state of a row as dc_feat_init leaves it (lane c of the row's LPR); first_pos: position
+// of the call's first row.
 template <int DTYPE, int D>
-__device__ __forceinline__ void init_row(const CommitArgs& a, int u, int slot, int j, const uint4& v,
-                                         int c) {
+__device__ __forceinline__ void init_row(const CommitArgs& a, int u, int slot, int first_pos, int j,
+                                         const uint4& v, int c) {
   using R = RowT<DTYPE, D>;
   float f[R::EPL];
   unpack_slice<DTYPE>(v, f);
@@ -196,7 +204,7 @@ __device__ __forceinline__ void init_row(const CommitArgs& a, int u, int slot, i
     a.alpha[i] = 0.0f;
     a.num[i] = 0.0;
     a.den[i] = 0.0;
-    a.pos[i] = a.next_pos + j;
+    a.pos[i] = first_pos + j;
     a.vnorm[i] = sqrtf(s);
     if (a.sigma) a.sigma[i] = 0.0f;
   }
@@ -215,6 +223,7 @@ __global__ void __launch_bounds__(RT) commit_path_kernel(CommitArgs a) {
   int t0, n;
   token_range(a.tok, b, t0, n);
   const int start = rows_before(a.unit_len, a.len, u), keep = rows_kept(a, b, n);
+  const int first_pos = a.next_pos - behind_of(a, u);
   for (int j0 = 0; j0 < keep; j0 += RPP) {
     const int j = j0 + jr;
     const bool on = j < keep;
@@ -232,11 +241,14 @@ __global__ void __launch_bounds__(RT) commit_path_kernel(CommitArgs a) {
       *reinterpret_cast<uint4*>((char*)a.k + to) = kw;
       *reinterpret_cast<uint4*>((char*)a.v + to) = vw;
     }
-    if (a.alpha && on) init_row<DTYPE, D>(a, u, start + j, j, vw, c);
+    if (a.alpha && on) init_row<DTYPE, D>(a, u, start + j, first_pos, j, vw, c);
   }
   if (a.unit_len) {
     __syncthreads();
-    if (threadIdx.x == 0) a.unit_len[u] = start + keep;
+    if (threadIdx.x == 0) {
+      a.unit_len[u] = start + keep;
+      store_behind(a, u, keep);
+    }
   }
 }
 
@@ -250,8 +262,9 @@ __global__ void __launch_bounds__(RT) commit_rows_kernel(CommitArgs a) {
   int t0, n;
   token_range(a.tok, b, t0, n);
   const int start = rows_before(a.unit_len, a.len, u), keep = rows_kept(a, b, n);
+  const int first_pos = a.next_pos - behind_of(a, u);
   for (int j = blockIdx.x * RPP + threadIdx.x / LPR; j < keep; j += gridDim.x * RPP)
-    init_row<DTYPE, D>(a, u, start + j, j,
+    init_row<DTYPE, D>(a, u, start + j, first_pos, j,
                        ldg16((const char*)a.v + (((size_t)u * a.cap + start + j) * LPR + c) * 16), c);
 }
 
@@ -261,7 +274,9 @@ __global__ void commit_len_kernel(CommitArgs a) {
   const int b = u / a.per_seq;
   int t0, n;
   token_range(a.tok, b, t0, n);
-  a.unit_len[u] = rows_before(a.unit_len, a.len, u) + rows_kept(a, b, n);
+  const int keep = rows_kept(a, b, n);
+  a.unit_len[u] = rows_before(a.unit_len, a.len, u) + keep;
+  store_behind(a, u, keep);
 }
 
 template <int DTYPE, int D>

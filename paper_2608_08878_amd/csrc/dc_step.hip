@@ -496,9 +496,9 @@ __device__ __forceinline__ void load_row_state(const DecodeArgs& a, size_t gi, R
 }
 
 // Feature update of one row from its weights: x in, the updated state in x and in
-// memory.
+// memory.  T, pmax: the unit's tokens_of and retired_pmax.
 template <int G>
-__device__ __forceinline__ void update_row(const DecodeArgs& a, size_t gi, bool is_new,
+__device__ __forceinline__ void update_row(const DecodeArgs& a, size_t gi, bool is_new, int T, int pmax,
                                            const float (&pj)[G], const float (&invl)[G],
                                            const float (&H)[G], float2 ret, float newnorm,
                                            RowState& x) {
@@ -509,14 +509,14 @@ __device__ __forceinline__ void update_row(const DecodeArgs& a, size_t gi, bool 
   float cz, cn;
   contrib_from_weights<G>(w, H, cz, cn);
   if (is_new) {
-    x = {cz * invG, newnorm, (double)cn, (double)cz, a.T - 1};
+    x = {cz * invG, newnorm, (double)cn, (double)cz, T - 1};
     a.pos[gi] = x.p;
     a.vnorm[gi] = x.vn;
   } else {
     x.al = (a.arec ? 0.0f : x.al) + cz * invG;
     x.de = x.de + (double)cz;
     x.nu = x.nu + (double)cn;
-    if (a.retire && x.p <= a.pmax_ret) {
+    if (a.retire && x.p <= pmax) {
       x.de = x.de - (double)ret.x;
       x.nu = x.nu - (double)ret.y;
     }
@@ -683,7 +683,9 @@ __device__ __forceinline__ void step_unit_body(const DecodeArgs& a, const EvictA
   if constexpr (FEAT) {
     const float newnorm = a.append ? new_row_vnorm<D>(a, u, &newnorm_slot) : 0.0f;
     const int newrow = a.append ? len_old_of(a, u) : -1;
-    const float invT = 1.0f / (float)a.T;
+    // (only ragged caches hold sequences of different counts)
+    const int T = RAG ? tokens_of(a, u) : a.T, pmax = RAG ? retired_pmax(a, u) : a.pmax_ret;
+    const float invT = 1.0f / (float)T;
     constexpr float invG = 1.0f / G;
     uint64_t* keys = reinterpret_cast<uint64_t*>(sbuf);   // row i's key replaces its weights
     // The rows of pass A's 64-row groups, one per lane: group b (wave b mod SNW)
@@ -714,7 +716,7 @@ __device__ __forceinline__ void step_unit_body(const DecodeArgs& a, const EvictA
       double nu = x.nu + (double)cn;
       int32_t ps = x.p;
       float vn = x.vn;
-      if (retire && ps <= a.pmax_ret) {
+      if (retire && ps <= pmax) {
         de = de - (double)rz;
         nu = nu - (double)rn;
       }
@@ -722,7 +724,7 @@ __device__ __forceinline__ void step_unit_body(const DecodeArgs& a, const EvictA
         al = cz * invG;
         de = (double)cz;
         nu = (double)cn;
-        ps = a.T - 1;
+        ps = T - 1;
         vn = newnorm;
       }
       if (!guard || valid) {
@@ -758,7 +760,7 @@ __device__ __forceinline__ void step_unit_body(const DecodeArgs& a, const EvictA
     }
     // the appended row's position and value norm (the other rows keep theirs)
     if (a.append && tid == 0) {
-      a.pos[ub + newrow] = a.T - 1;
+      a.pos[ub + newrow] = T - 1;
       a.vnorm[ub + newrow] = newnorm;
     }
     if (a.window > 0) write_ring2<D, G>(a, u, M, invl, H);
@@ -1014,6 +1016,7 @@ __global__ void __launch_bounds__(SNT, FEW || !FEAT ? 1 : G > 4 ? 6 : 8) stepc_d
     H[j] = comb[2][j];
   }
   if constexpr (FEAT) {
+    const int T = tokens_of(a, u), pmax = retired_pmax(a, u);
     auto update = [&](int i0) {
 #pragma unroll
       for (int k = 0; k < RB; ++k) {
@@ -1022,11 +1025,11 @@ __global__ void __launch_bounds__(SNT, FEW || !FEAT ? 1 : G > 4 ? 6 : 8) stepc_d
         float pj[G];
 #pragma unroll
         for (int j = 0; j < G; ++j) pj[j] = __builtin_amdgcn_exp2f((sj[k][j] - M[j]) * LOG2E);
-        update_row<G>(a, ub + i, i == newrow, pj, invl, H, ret[k], newnorm, x[k]);
+        update_row<G>(a, ub + i, i == newrow, T, pmax, pj, invl, H, ret[k], newnorm, x[k]);
       }
     };
     auto score = [&](int i0) {            // (past the last row of a chunk the state is that of its last row)
-      const float invT = 1.0f / (float)a.T;
+      const float invT = 1.0f / (float)T;
       float f[RB][4], sc[RB];
 #pragma unroll
       for (int k = 0; k < RB; ++k) make_features(x[k].al, x[k].vn, x[k].nu, x[k].de, x[k].p, invT, f[k]);
