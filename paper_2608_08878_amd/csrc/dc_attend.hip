@@ -77,7 +77,8 @@ __device__ __forceinline__ float rescale(float m, float mn) {
 
 // A row keeps its maximum while no key exceeds it by more than this (in powers of two): weights are
 // then at most 2^SLACK instead of 1, which float32 sums and bf16 weights hold as well, and the
-// accumulators are rescaled once or twice in a long row instead of at every new maximum.
+// accumulators are rescaled once or twice in a long row instead of at every new maximum.  Values near the
+// type's largest can overflow by it; the pass that follows a result that is not finite keeps none.
 constexpr float SLACK = 8.0f;
 
 // Key held by accumulator register i of a lane in half h of the wave: bit i of a 32-key block.
@@ -470,7 +471,7 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
   const float c = a.scale * LOG2E;
   f32x16_t o[D / 32];
   float m, l;
-  // One pass over the keys.  CAREFUL: masked blocks go key by key.
+  // One pass over the keys.  CAREFUL: masked blocks go key by key, and weights are at most 1.
   auto pass = [&](auto careful) DC_INLINE {
     constexpr bool CAREFUL = decltype(careful)::value;
     m = NEG_INF;
@@ -501,7 +502,7 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
       const float mn = fmaxf(m, half_max(mx) * c);
-      if (__any(mn > m + SLACK)) {
+      if (__any(mn > m + (CAREFUL ? 0.0f : SLACK))) {
         const float f = rescale(m, mn);
         l *= f;
 #pragma unroll
@@ -531,7 +532,8 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
     }
   };
   pass(std::false_type{});
-  // Again, carefully, only if a masked value row was met that is not finite (0 times it is NaN).
+  // Again, carefully, only if a masked value row was met that is not finite (0 times it is NaN), or the
+  // sums left float32's range.
   float z = 0.0f;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)

@@ -3,12 +3,13 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import prompt as op
 from oracle import select as osel
 from oracle import unit as ounit
 from paper_2608_08878_amd.buffers import DecodeBuffers, make_policy, make_tokens
 
 from . import harness as H
-from .test_gpu_prompt import Cache
+from .test_gpu_prompt import Cache, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -34,6 +35,26 @@ def test_a_captured_attention_keeps_its_workspace():
         assert torch.equal(out, want)
         assert all((x == 255).all() for x in taken)
         assert torch.equal(c.buf.prompt_attention(c.tokens, c.q), want)     # eager, in the present one
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("counts,rows,hk", [([130] * 12, 300, 8), ([60] * 40, 300, 8), ([3], 300, 1), ([8] * 64, 300, 8)])
+def test_values_near_the_largest_number(dtype, tree, counts, rows, hk):
+    # one key 7.5 powers of two above all others, its value 3e36: the output is finite, though 2^7.5 of it
+    # leave float32's range
+    c = Cache(counts, rows, dtype, 128, hk, 1, seed=70)
+    c.q.fill_(1.0)
+    c.buf.k.zero_()
+    c.buf.k[:, 200] = 7.5 * np.log(2) * 128 ** 0.5 / 128
+    c.buf.v[:, 200] = 3e36
+    if tree:
+        out = c.buf.tree_attention(c.tokens, torch.full((c.N,), -1, dtype=torch.int32, device="cuda"), c.q)
+        masks = [op.tree_mask([-1] * n) for n in counts]
+    else:
+        out, masks = c.buf.prompt_attention(c.tokens, c.q), [op.causal_mask(n) for n in counts]
+    assert torch.isfinite(out.float()).all()
+    check_attention(c, out, 0, masks)
 
 
 # ------------------------------------------- sequences that see different numbers of tokens
