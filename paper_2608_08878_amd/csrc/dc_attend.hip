@@ -367,6 +367,7 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const Place& w, 
     for (int y = 0; y < 4; ++y)
       *reinterpret_cast<float4*>(st + (q * CH + ((8 * db + 2 * y + h) ^ (q & (CH - 1)))) * 16) =
           make_float4(o[db][4 * y] * inv, o[db][4 * y + 1] * inv, o[db][4 * y + 2] * inv, o[db][4 * y + 3] * inv);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all pieces are in LDS before other lanes read them
   auto chunk = [&](int r, int c) DC_INLINE {
     return *reinterpret_cast<const float4*>(st + (r * CH + (c ^ (r & (CH - 1)))) * 16);
   };
