@@ -594,7 +594,8 @@ size_t dc_tokens_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, i
  *          takes feat->behind.
  * K and V of the path move in place.  Afterwards unit_len[u] += rows kept, kv->len +=
  * width, feat->next_pos += width, and a sequence's T by the rows that it keeps (host: the
- * caller may lower kv->len to any bound of the unit lengths that it knows).
+ * caller may lower kv->len to any bound of the unit lengths that it knows, and has to where
+ * keep lets the lengths fall behind it until it reaches the capacity).
  * A unit may stay at 0 rows (an empty prompt of a batch): the next step's append is its first
  * row; a step without an append takes at least one.
  * Equal counts need nothing else; cu or keep make the units' lengths differ, which

@@ -317,6 +317,16 @@ class DecodeBuffers:
             self._ints(keep, (self.dims.batch,), "keep")
         B.dc_commit_rows(self.dims, self.kv, self.feat, tokens, path, keep, width, self._stream_here(stream))
 
+    def tighten_len(self, stream=None) -> int:
+        """The bound of the units' rows down to the longest unit's.  commit_rows counts a call's full
+        width, as it reads nothing back; where fewer rows stay, the bound would reach the capacity of a
+        cache with room, and calls are planned for rows that are not there.  Waits for the stream."""
+        if self.unit_len is not None:
+            with torch.cuda.stream(stream):            # (None: the current one)
+                rows = int(self.unit_len.max())
+            self.kv.len = max(0, min(self.kv.len, rows))
+        return self.kv.len
+
     def prefill(self, tokens, rope, q, k, v, pos, layer=0, out=None, stream=None):
         """One layer of a prompt: norm, rotation, the rows into the cache, attention.  After
         the last layer commit_rows(tokens) makes the rows part of the cache."""

@@ -35,3 +35,18 @@ def test_they_add_up_to_less_than_the_present_one():
     assert sum(held) < 2 * buf.ws_bytes == 2 * held[-1]
     need = B.dc_tokens_workspace_bytes(buf.dims, B.dc_tokens(200, 200, None), 40000)
     assert need <= buf.ws_bytes and buf.ws.data_ptr() % 16 == 0
+
+
+def test_the_bound_of_the_rows_comes_down_to_the_longest_unit():
+    buf = DecodeBuffers(2, 1, 8, 2, 64, 100, features=False, ragged=True, device="cpu")
+    buf.kv.len = 90
+    buf.unit_len[:] = 40
+    buf.unit_len[2] = 63
+    assert buf.tighten_len() == 63 == buf.kv.len
+    buf.unit_len[2] = 95                                # past the bound: calls clamp to it
+    assert buf.tighten_len() == 63
+    buf.unit_len.zero_()
+    assert buf.tighten_len() == 0
+    even = DecodeBuffers(1, 1, 8, 2, 64, 100, features=False, device="cpu")
+    even.kv.len = 12
+    assert even.tighten_len() == 12

@@ -6,6 +6,7 @@ import torch
 from oracle import prompt as op
 from oracle import select as osel
 from oracle import unit as ounit
+from paper_2608_08878_amd import binding as B
 from paper_2608_08878_amd.buffers import DecodeBuffers, make_policy, make_tokens
 
 from . import harness as H
@@ -35,6 +36,26 @@ def test_a_captured_attention_keeps_its_workspace():
         assert torch.equal(out, want)
         assert all((x == 255).all() for x in taken)
         assert torch.equal(c.buf.prompt_attention(c.tokens, c.q), want)     # eager, in the present one
+
+
+def test_short_paths_fill_a_cache_to_its_capacity():
+    # 8 drafted tokens a step, of which one or two stay: more steps than the capacity holds drafts
+    c = Cache([8, 8], 20, "bf16", 64, 1, 2, seed=51, spare=40, lens=[20, 20])        # capacity 68
+    buf, path = c.buf, torch.tensor([[1, 4], [0, 3]], dtype=torch.int32, device="cuda")
+    keep = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    chain = torch.arange(-1, 7, dtype=torch.int32, device="cuda").repeat(2)
+    lens = [20, 20]
+    for step in range(20):
+        new = buf.k[torch.arange(2), torch.tensor([n + p for n, p in zip(lens, (1, 0))])].clone()
+        c.lens = lens
+        check_attention(c, buf.tree_attention(c.tokens, chain, c.q), 0, [op.causal_mask(8)] * 2)
+        buf.commit_rows(c.tokens, path, keep)
+        assert buf.tighten_len() == lens[0] + 2 == buf.unit_len.max()
+        assert torch.equal(buf.k[torch.arange(2), torch.tensor(lens)], new)
+        lens = [lens[0] + 2, lens[1] + 1]
+    assert buf.unit_len.tolist() == lens == [60, 40]
+    with pytest.raises(B.DCError):                      # 60 rows and 8 tokens are the capacity's 68
+        buf.commit_rows(make_tokens([9, 9]), width=1)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
