@@ -714,7 +714,12 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   // 1.3 alone on a CU and 2 beside another (bf16, 128 elements), joined outputs at 3.5 TB/s.  One prompt
   // of 512 tokens 21 -> 16 us against as many parts as fit, of 1024 37 -> 27; 256 behind 16384 rows
   // 94, with half as many parts 102, in one 330.
-  const int per_cu = bm == 128 || (dtype == 1 && D == 64) ? 2 : 1;
+  // Workgroups that a CU holds (Cfg::WAVES): two, but one of the small tiles whose buffers are a CU's LDS
+  // (float32, and bf16 with 128 elements) and of the 128-row float32 tiles with 128 elements, whose
+  // registers are a CU's.  For those one against two: 1000 tokens of 32/8 heads 151 and 169 us, 64 tokens
+  // of 8 sequences behind 4096 rows 326 and 353; where two parts are a few workgroups more than one
+  // round it is the slower (3 x 700 tokens behind 900 rows of 8/4 heads 234 and 203).
+  const int per_cu = dtype == 1 ? (bm == 128 || D == 64 ? 2 : 1) : bm == 128 && D == 64 ? 2 : 1;
   int64_t most = per_cu * CUS / tiles(bm);
   most = most > parts ? parts : most;
   most = most > MAX_PARTS ? MAX_PARTS : most < 1 ? 1 : most;

@@ -50,3 +50,11 @@ def test_the_bound_of_the_rows_comes_down_to_the_longest_unit():
     even = DecodeBuffers(1, 1, 8, 2, 64, 100, features=False, device="cpu")
     even.kv.len = 12
     assert even.tighten_len() == 12
+
+
+def test_float32_heads_of_128_are_cut_for_one_workgroup_a_cu():
+    # 300 tokens of 32/8 heads: 80 tiles of 128 rows; the parts' outputs and statistics in float32
+    dims = B.dc_dims(1, 1, 32, 8, 128, 20000, B.DC_F32, 0, 0.0)
+    each = 300 * 32 * (128 + 2) * 4
+    for rows in (5000, 16300):
+        assert 0 < B.dc_tokens_workspace_bytes(dims, B.dc_tokens(300, 300, None), rows) <= 256 // 80 * each + 255
