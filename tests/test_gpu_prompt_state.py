@@ -10,7 +10,7 @@ from paper_2608_08878_amd import binding as B
 from paper_2608_08878_amd.buffers import DecodeBuffers, make_policy, make_tokens
 
 from . import harness as H
-from .test_gpu_prompt import Cache, check_attention
+from .test_gpu_prompt import MANY, Cache, check_attention, close, random_tree, uneven
 
 pytestmark = pytest.mark.gpu
 
@@ -76,6 +76,33 @@ def test_values_near_the_largest_number(dtype, tree, counts, rows, hk):
         out, masks = c.buf.prompt_attention(c.tokens, c.q), [op.causal_mask(n) for n in counts]
     assert torch.isfinite(out.float()).all()
     check_attention(c, out, 0, masks)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("counts,rows,hk,G,lens", MANY)
+def test_trees_of_many_rows_do_not_depend_on_other_branches(dtype, D, counts, rows, hk, G, lens):
+    # every tile shape: a node's rows infinite or NaN, which reaches the nodes below it alone
+    if max(counts) > 256:
+        counts = [256, 17]
+    print(f"branches {dtype} D={D} counts={counts[:4]}", flush=True)
+    c = Cache(counts, rows, dtype, D, hk, G, 1, uneven(len(counts) * hk, rows) if lens else None, seed=rows + D)
+    parents = [random_tree(n, 5 * b + n) for b, n in enumerate(counts)]
+    flat = torch.tensor(sum(parents, []), dtype=torch.int32, device="cuda")
+    want = c.buf.tree_attention(c.tokens, flat, c.q)
+    for b, _, n in c.spans():
+        for h in range(hk if n else 0):
+            u = c.unit(b, 0, h)
+            at = c.lens[u] + n // 2
+            c.buf.v[u, at] = float("inf") if h % 2 else float("nan")
+            c.buf.k[u, at] = float("nan") if h % 2 else -float("inf")
+    got = c.buf.tree_attention(c.tokens, flat, c.q)
+    for b, t0, n in c.spans():
+        if n == 0:
+            continue
+        sees = torch.from_numpy(op.tree_mask(parents[b])[:, n // 2].copy()).cuda()
+        g, w = got[t0:t0 + n], want[t0:t0 + n]
+        assert close(g[~sees], w[~sees], rows + max(counts), 6, dtype), b
+        assert not torch.isfinite(g[sees].float()).any(), b
 
 
 # ------------------------------------------- sequences that see different numbers of tokens
