@@ -500,11 +500,17 @@ dc_status dc_reinforce_terms(int32_t steps, int32_t rollouts, const dc_reinforce
  * is not committed leaves the cache as it was (a decode step overwrites the slots).
  * Both dtypes, ragged caches in float32 too (which dc_decode_step does not take).
  * Model weights are frozen in this method: these are forward passes only.
+ * They are no decode steps to the feature state: their attention adds nothing to alpha, sigma or the
+ * entropy window, and the commit does not advance dc_feat.step.  Committed rows start as
+ * dc_feat_init's do; the rows that drafts looked at have the features of the decode steps alone, so
+ * accepted drafts leave other scores than the same tokens one step at a time.
  */
 
 /* The tokens of one call, packed: those of sequence b are cu[b] .. cu[b + 1] - 1 of N.
  * A sequence may have none.  Offsets on the device that are not ascending in
- * [0, tokens], or counts over max_tokens, are clamped. */
+ * [0, tokens], or counts over max_tokens, are clamped.  Tokens before cu[0] or from cu[batch] on
+ * (padding) belong to no sequence: dc_qk_norm_rope turns their heads like the others' (their
+ * positions are read) and writes none to the cache, the attentions leave their rows of out. */
 typedef struct {
   int32_t tokens;       /* N, 1 .. 2^25 */
   int32_t max_tokens;   /* host: the most tokens of one sequence (1..tokens) */
@@ -512,7 +518,8 @@ typedef struct {
                            batch * max_tokens) */
 } dc_tokens;
 
-/* Norm and rotation of a head x[head_dim], in float32 with one rounding at the end:
+/* Norm and rotation of a head x[head_dim], in float32 (squares included: elements up to
+ * 1e18) with one rounding at the end:
  *   norm = 1: x <- x / sqrt(mean(x^2) + eps) * gain (NULL: ones); norm = 0: x as it is;
  *   then pair i < rot_dim / 2 of its elements, (i, i + rot_dim / 2) or with interleaved
  *   (2 i, 2 i + 1), turns by phi = position * inv_freq[i]:
@@ -551,9 +558,16 @@ dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
  * slots behind the rows hold the tokens' own K/V (dc_qk_norm_rope): token r of a sequence
  * sees the unit's rows and the tokens 0..r.
  *   q    [N][n_q_heads][head_dim], dtype, contiguous
- *   out  the same shape: o = sum_i a_i v_i, a = softmax_i(scale q.k_i); not q itself
- * Slots that a token does not see have no influence on it, whatever they hold.
- * Workspace: dc_tokens_workspace_bytes(dims, tokens, kv->len + max_tokens) bytes.
+ *   out  the same shape: o = sum_i a_i v_i, a = softmax_i(scale q.k_i); overlaps neither q nor
+ *        the cache
+ * Scores, maxima and sums are float32.  With DC_BF16 the weights exp(s - m), m a running maximum,
+ * meet the values in bf16 (2^-8 of each at most), and the sum that divides is of the rounded ones:
+ * relative errors of about 0.0018 where the output's own rounding alone gives 0.0016.  The sum over
+ * the keys of weights of at most 1 times the values has to stay within float32 before the division.
+ * Slots that a token does not see have no influence on it beyond the order of its sums, whatever
+ * they hold.
+ * Workspace: dc_tokens_workspace_bytes(dims, tokens, kv->len + max_tokens) bytes, the call's alone
+ * until it has run: calls on other streams, and graphs that may replay at the same time, take others.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_CAPACITY, DC_ERR_WORKSPACE,
  * DC_ERR_UNSUPPORTED (alignment, grids past 2^24 workgroups: batch x KV heads x tiles of
  * 32 to 128 (token, head) rows of the longest sequence). */

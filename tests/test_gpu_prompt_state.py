@@ -7,7 +7,7 @@ from oracle import prompt as op
 from oracle import select as osel
 from oracle import unit as ounit
 from paper_2608_08878_amd import binding as B
-from paper_2608_08878_amd.buffers import DecodeBuffers, make_policy, make_tokens
+from paper_2608_08878_amd.buffers import DecodeBuffers, make_policy, make_rope, make_tokens
 
 from . import harness as H
 from .test_gpu_prompt import MANY, Cache, check_attention, close, random_tree, uneven
@@ -76,6 +76,40 @@ def test_values_near_the_largest_number(dtype, tree, counts, rows, hk):
         out, masks = c.buf.prompt_attention(c.tokens, c.q), [op.causal_mask(n) for n in counts]
     assert torch.isfinite(out.float()).all()
     check_attention(c, out, 0, masks)
+
+
+def test_padding_around_the_sequences_is_left():
+    # two tokens before the first sequence and three behind the last
+    c = Cache([5, 0, 9], 40, "bf16", 128, 2, 4, seed=71, lens=[40, 38, 40, 40, 7, 30])
+    t = make_tokens([5, 0, 9])
+    t.tokens = 19
+    t.cu_tensor.copy_(torch.tensor([2, 7, 7, 16], dtype=torch.int32))
+    wide = [torch.randn((19, h, 128), generator=c.g).to(c.td).cuda() for h in (8, 2, 2)]
+    pos = torch.randint(0, 900, (19,), generator=c.g, dtype=torch.int32).cuda()
+    rope = make_rope(torch.rand(64, generator=c.g).cuda(), norm=True)
+    tight = [x[2:16].contiguous() for x in wide]
+    want, _ = c.buf.norm_rope(c.tokens, rope, *tight, pos[2:16].contiguous())
+    k, v = c.buf.k.clone(), c.buf.v.clone()
+    for u, r in enumerate(c.lens):
+        n = [5, 0, 9][u // 2]
+        c.buf.k[u, r:r + n], c.buf.v[u, r:r + n] = 3, 4
+    got, _ = c.buf.norm_rope(t, rope, *wide, pos)
+    assert torch.equal(got[2:16], want) and torch.equal(c.buf.k, k) and torch.equal(c.buf.v, v)
+    heads = [x.contiguous() for x in (got[:2], got[16:])]
+    for x, at in zip(heads, (slice(0, 2), slice(16, 19))):          # the padding's heads are turned like any
+        one = make_tokens([x.shape[0]])
+        alone = DecodeBuffers(1, 1, 8, 2, 128, 8, "bf16", features=False)
+        assert torch.equal(alone.norm_rope(one, rope, wide[0][at], wide[1][at], None, pos[at].contiguous())[0], x)
+    parent = torch.full((19,), -1, dtype=torch.int32, device="cuda")
+    for tree in (False, True):
+        out = torch.full((19, 8, 128), 5.0, dtype=c.td, device="cuda")
+        a = c.buf.tree_attention(t, parent, got, out=out) if tree else c.buf.prompt_attention(t, got, out=out)
+        b = c.buf.tree_attention(c.tokens, parent[:14].contiguous(), want) if tree else \
+            c.buf.prompt_attention(c.tokens, want)
+        assert (a[:2] == 5).all() and (a[16:] == 5).all()
+        assert close(a[2:16], b, 50, float(c.buf.v.abs().max()), "bf16")
+    c.buf.commit_rows(t)
+    assert c.buf.unit_len.tolist() == [45, 43, 40, 40, 16, 39]
 
 
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
