@@ -399,13 +399,20 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const Place& w, 
   }
 }
 
-// Bound by the matrix cores and, at that, by power: two prompts of 8192 tokens (32/8 heads of 128) 1045 us =
-// 1.05 PFLOP/s at a clock of 1.8 GHz, where a large library product reaches 1.35; on zeros 860.  Two waves a
-// SIMD (256 registers each; one wave 1861) overlap one's softmax with the other's products.  Tried and not
-// kept: three key blocks in hand in a wave 1075-1086, 64 rows a wave 1455, eight waves a workgroup 1105, tiles
-// of 32 keys 1112.  With 64-element heads the exponentials bound it (4 x 2048 tokens, 64/8 heads: 180 us =
-// 0.76 PFLOP/s; tiles of 128 keys 209).  Few rows over long caches are bound by HBM: 160 drafted
-// tokens over 16 caches of up to 16384 rows, 834 MB, 171-178 us (its loads alone 149).
+// Two prompts of 8192 tokens (32/8 heads of 128) 1045-1090 us = 1.0 PFLOP/s, where a large library product
+// reaches 1.35: matrix cores busy 52 % of the cycles, vector instructions issued in 47 %, at a clock that the
+// card's power holds at 1.6 to 1.8 GHz (the call on zeros 860).  Two waves a SIMD (256 registers each; one wave
+// 1861) overlap one's softmax with the other's products.  Tried and not kept: three key blocks in hand in a
+// wave 1075-1086, 64 rows a wave 1455, eight waves a workgroup 1105, tiles of 32 keys 1112.  64-element heads
+// (4 x 2048 tokens, 64/8 heads, 180 us = 0.76 PFLOP/s; tiles of 128 keys 209) take twice the exponentials for a
+// product: vector instructions in 64 %, matrix cores 37 %, and most products come right behind a wait for
+// their operands from LDS.
+// The compiler cannot see that the wait at a step's head covers the Q rows' loads too, and waits for them again
+// before the step's first products, which by then is a wait for the next tile.  Prompts do not show it: built
+// with those waits ahead of the loop they take the same (8192 tokens 1044 us, 64 elements 178), the tiles being
+// in the L2.  Drafts over caches in HBM do: 320 tokens over 16 caches of up to 16384 rows, 834 MB, 171-178 us,
+// without the waits 163.  The rest of that call is the lengths: parts are cut by the longest cache, so the
+// shorter ones' last workgroups leave at once (16 caches of 16384 rows, 1.07 GB, one token each: 171).
 template <int DT, int D, int RW, int KW, int SK, bool TREE>
 __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES)) attend_kernel(AttendArgs a) {
   using T = KVT<DT, D>;
@@ -479,7 +486,7 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
     l = 0.0f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16_t{};
-    // a tile in buffer BUF; the next one's loads are under way meanwhile
+    // a tile in buffer BUF; the next one's loads go out first
     auto tile_step = [&](int it, auto bufc) DC_INLINE {
       constexpr int BUF = decltype(bufc)::value;
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
@@ -741,8 +748,8 @@ bool attend_plan(AttendArgs& a, int dtype, int D, int L) {
   a.most_splits = (int)most;
   const int64_t nt = (rows + bm - 1) / bm;
   a.bm = bm;
-  // Rows that one row tile reads, once, and that no cache holds anyway: non-temporal (16 x 32 drafted
-  // tokens over 16k rows, 834 MB, 191 -> 180 us; 13 over 4k rows, 17 MB, 15.6 -> 16.8)
+  // Rows that one row tile reads, once, and that no cache holds anyway: non-temporal (320 drafted
+  // tokens of 16 sequences over up to 16k rows, 834 MB, 191 -> 180 us; 13 over 4k rows, 17 MB, 15.6 -> 16.8)
   a.once = nt == 1 && bytes > BIG_CACHE;
   a.splits = (int)splits;
   a.chunk = (int)chunk;

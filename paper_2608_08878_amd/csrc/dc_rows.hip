@@ -36,8 +36,8 @@ __device__ __forceinline__ uint4 pack_slice(const float* f) {
 // One token and one row per lane group where that makes no more than FEW_WGS workgroups, else TPB
 // tokens: a workgroup's angles and places are a chain of loads before its first store, which many
 // small ones repeat and few large ones show (32 + 16 heads of 128, one token at a time and by four:
-// 64 tokens 4.3 and 12.7 us, 1024 9.2 and 15.6, 4096 29.9 and 31.4, 20001 142 and 107).
-// 20001 tokens, 481 MB, 107 us = 4.5 TB/s, of the 4.8 that a copy reaches.
+// 64 tokens 4.3 and 12.7 us, 1024 9.2 and 15.6, 4096 29.9 and 31.4, 19564 142 and 107).
+// 19564 tokens, 481 MB, 107 us = 4.5 TB/s, of the 4.8 that a copy reaches.
 constexpr int TPB = 4;               // (a wave each for their places)
 constexpr int FEW_WGS = 16384;
 static_assert(TPB * 64 <= RT, "a wave per token");
