@@ -136,8 +136,8 @@ typedef struct {
                           holds by how many tokens every unit's sequence is behind next_pos:
                           its own T, the position of its next token and the T of its pos / T
                           are next_pos less that.  NULL, and row 0: all are at next_pos. */
-  int32_t behind_row;  /* host: the row in force, 0 for none.  Setting next_pos by hand puts
-                          every sequence at that T (row 0) */
+  int32_t behind_row;  /* host: the row in force, 0 for none.  Setting next_pos to another
+                          value by hand puts every sequence at that T (row 0) */
   int32_t behind_at;   /* host: the next_pos that behind_row belongs to */
   int32_t ring_row[DC_MAX_WINDOW];  /* host: per ring slot, the row in force at that step */
 } dc_feat;
@@ -541,14 +541,14 @@ typedef struct {
  *      t * ld (ld >= heads * head_dim: parts of a fused projection are read in place)
  *   pos    device [N] int32: the tokens' positions (NULL if rot_dim = 0)
  *   q_out  [N][n_q_heads][head_dim] contiguous; may be q itself if ld_q = n_q_heads *
- *          head_dim, and overlaps no input otherwise
+ *          head_dim, and overlaps no input otherwise, nor k_out
  *   k_out  NULL: the rotated keys and the values go to the slots behind the rows of
  *          layer `layer` of kv; else [N][n_kv_heads][head_dim] contiguous (may be k
  *          likewise), v and kv are not used and may be NULL: with q_out
  *          the inputs of dc_decode_step for one token per sequence and one layer.
  * Rows and pointers are multiples of 16 bytes.  dims.capacity >= kv->len + max_tokens.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE (sizes, layer, ld), DC_ERR_CAPACITY, DC_ERR_VALUE
- * (eps, flags), DC_ERR_UNSUPPORTED (rot_dim, alignment). */
+ * (eps, flags), DC_ERR_UNSUPPORTED (rot_dim, alignment, overlaps). */
 dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
                           const dc_tokens *tokens, const dc_rope *rope, const void *q, int64_t ld_q,
                           const void *k, int64_t ld_k, const void *v, int64_t ld_v,
@@ -569,7 +569,7 @@ dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
  * Workspace: dc_tokens_workspace_bytes(dims, tokens, kv->len + max_tokens) bytes, the call's alone
  * until it has run: calls on other streams, and graphs that may replay at the same time, take others.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_CAPACITY, DC_ERR_WORKSPACE,
- * DC_ERR_UNSUPPORTED (alignment, grids past 2^24 workgroups: batch x KV heads x tiles of
+ * DC_ERR_UNSUPPORTED (alignment, q and out overlap, grids past 2^24 workgroups: batch x KV heads x tiles of
  * 32 to 128 (token, head) rows of the longest sequence). */
 dc_status dc_prompt_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer,
                               const dc_tokens *tokens, const void *q, void *out, void *ws,

@@ -862,6 +862,14 @@ constexpr int MAX_TOKENS = 1 << 25;     // of one call
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// Whether n rows of `width` elements, ld from row to row, and m rows of another array share bytes.
+bool overlap(const dc_dims* d, const void* a, int64_t n, int64_t lda, int64_t wa, const void* b, int64_t m,
+             int64_t ldb, int64_t wb) {
+  const int64_t e = d->dtype == DC_BF16 ? 2 : 4;
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + (uintptr_t)(((m - 1) * ldb + wb) * e) && y < x + (uintptr_t)(((n - 1) * lda + wa) * e);
+}
+
 dc_status check_tokens(const dc_dims* dims, const dc_tokens* t) {
   const dc_status st = check_dims(dims);
   if (st != DC_OK) return st;
@@ -918,6 +926,8 @@ dc_status attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_t
   if (!plan_attend(dims, tokens, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
   if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
   if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  const int64_t width = (int64_t)a.hq * dims->head_dim;
+  if (overlap(dims, q, tokens->tokens, width, width, out, tokens->tokens, width, width)) return DC_ERR_UNSUPPORTED;
   a.q = q;
   a.out = out;
   a.k = kv->k;
@@ -960,6 +970,16 @@ dc_status dc_qk_norm_rope(const dc_dims* dims, const dc_kv* kv, int32_t layer,
       !aligned16(q_out) || !aligned16(cache ? v : k_out))
     return DC_ERR_UNSUPPORTED;
   if ((q == q_out && ld_q != wq) || (!cache && k == k_out && ld_k != wk)) return DC_ERR_UNSUPPORTED;
+  // outputs in place or apart from everything that is read (a row of one is written before others are read)
+  const int64_t N = tokens->tokens;
+  auto meets = [&](const void* out, int64_t w, const void* in, int64_t ld, int64_t wi, bool in_place) {
+    return !(in_place && in == out) && overlap(dims, out, N, w, w, in, N, ld, wi);
+  };
+  if (meets(q_out, wq, q, ld_q, wq, true) || meets(q_out, wq, k, ld_k, wk, false) ||
+      (cache && meets(q_out, wq, v, ld_v, wk, false)) ||
+      (!cache && (meets(k_out, wk, q, ld_q, wq, false) || meets(k_out, wk, k, ld_k, wk, true) ||
+                  meets(k_out, wk, q_out, wq, wq, false))))
+    return DC_ERR_UNSUPPORTED;
   dc::NormRopeArgs a;
   memset(&a, 0, sizeof(a));
   a.q = q;
