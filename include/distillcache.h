@@ -137,7 +137,8 @@ typedef struct {
                           its own T, the position of its next token and the T of its pos / T
                           are next_pos less that.  NULL, and row 0: all are at next_pos. */
   int32_t behind_row;  /* host: the row in force, 0 for none.  Setting next_pos to another
-                          value by hand puts every sequence at that T (row 0) */
+                          value by hand puts every sequence at that T (row 0); a caller who goes
+                          back to an earlier state sets behind_row and behind_at with it */
   int32_t behind_at;   /* host: the next_pos that behind_row belongs to */
   int32_t ring_row[DC_MAX_WINDOW];  /* host: per ring slot, the row in force at that step */
 } dc_feat;
