@@ -621,6 +621,112 @@ size_t dc_tokens_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, i
 dc_status dc_commit_rows(const dc_dims *dims, dc_kv *kv, dc_feat *feat, const dc_tokens *tokens,
                          const int32_t *path, const int32_t *keep, int32_t width, void *hip_stream);
 
+/* ---- Rows that sequences share, and blocks of rows ------------------------
+ *
+ * Caches that a step should not read once per sequence, or not whole: the rollouts of one
+ * prompt (Sec. 3.2: K sampled rollouts per prompt, each with its teacher) have the prompt's rows in common, and
+ * the teacher's caches and the heads that the hybrid leaves unpruned only grow.  As the entry points
+ * for several tokens at once: token r of a sequence is row rows + r of its units, written there by
+ * dc_qk_norm_rope, and part of the cache with dc_commit_rows; one token per
+ * sequence is a decode step.  Forward passes only, both dtypes, ragged caches too, and no decode
+ * steps to the feature state.
+ */
+
+/* Rows in common.  Prefix p is a cache of its own, unit (p * n_layers + l) * n_kv_heads + g, of the same
+ * heads, head_dim and dtype as the sequences' caches. */
+typedef struct {
+  const dc_kv *kv;        /* k, v [prefixes * n_layers * n_kv_heads][capacity][head_dim]; len (0: no rows) and
+                             unit_len as for every cache, units of 0 rows included */
+  int32_t capacity;       /* rows allocated per unit */
+  int32_t prefixes;       /* >= 1 */
+  int32_t max_members;    /* host: the most sequences of one prefix (1..batch) */
+  const int32_t *first;   /* device [prefixes + 1]: prefix p is that of sequences first[p] .. first[p + 1] - 1,
+                             ascending in [0, batch] (a prefix may have none; a sequence before first[0] or from
+                             first[prefixes] on has no prefix), or NULL: max_members each (prefixes * max_members =
+                             batch).  Other values are clamped to stay in the buffers, the outputs of their
+                             sequences unspecified. */
+} dc_shared;
+
+/* dc_prompt_attention (parent NULL) or dc_tree_attention of sequences that have rows in common: a token
+ * sees its prefix's rows, its unit's rows, and its sequence's tokens as there.  The prefix's rows are
+ * read for all its sequences together.
+ * Workspace: dc_shared_workspace_bytes(dims, tokens, shared, kv->len + max_tokens) bytes, as for
+ * dc_prompt_attention the call's alone until it has run.
+ * Errors: those of dc_prompt_attention, dc_tree_attention; DC_ERR_NULL (shared, its cache), DC_ERR_SHAPE (its
+ * sizes), DC_ERR_UNSUPPORTED (its alignment, more than 2^24 units). */
+dc_status dc_shared_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer, const dc_tokens *tokens,
+                              const int32_t *parent, const dc_shared *shared, const void *q, void *out,
+                              void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Workspace bytes of dc_shared_attention for prefixes of up to shared->kv->len rows (no pointer but kv is
+ * read) and caches of up to max_len rows, the tokens' own included.  0 for invalid sizes.  It does not
+ * shrink where the lengths grow. */
+size_t dc_shared_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, const dc_shared *shared,
+                                 int32_t max_len);
+
+/* Blocks of a cache: block j of a unit is its rows j * rows .. (j + 1) * rows - 1, complete when the unit
+ * holds them all. */
+typedef struct {
+  int32_t rows;      /* 16, 32, 64 or 128 */
+  void *bounds;      /* [units][capacity / rows][2][head_dim], dtype: element by element the largest and the
+                        smallest of the block's keys (infinite ones and NaN as the type's largest finite
+                        numbers of their sign).  NULL if capacity < rows. */
+} dc_blocks;
+
+/* Brings the bounds up to date, all layers: those of every complete block that holds a row from `from`
+ * on are computed from its keys, the others left as they are.  After dc_commit_rows (or a
+ * decode step) `from` is the rows that every unit had before; after an eviction, which moves
+ * rows, 0.
+ * Errors: DC_ERR_NULL, DC_ERR_SHAPE (from outside 0..kv->len), DC_ERR_UNSUPPORTED (rows, alignment). */
+dc_status dc_block_bounds(const dc_dims *dims, const dc_kv *kv, const dc_blocks *blocks, int32_t from,
+                          void *hip_stream);
+
+/* Most blocks of a list. */
+#define DC_MAX_CHOSEN 2048
+
+/* A choice: every `share` successive tokens of a sequence (the last ones may be fewer) choose `count`
+ * blocks for each KV head together.  Lists are [batch][groups][n_kv_heads][count] int32, groups =
+ * ceil(max_tokens / share): group i of a sequence is its tokens i * share .. */
+typedef struct {
+  int32_t count;         /* 1..DC_MAX_CHOSEN */
+  int32_t share;         /* >= 1; 1: every token chooses alone */
+  int32_t first, last;   /* complete blocks that are always among them: the first and the last ones
+                            (first + last <= count) */
+} dc_pick;
+
+/* Chooses among the blocks that are complete in the rows before the call's tokens: the `first` and
+ * `last` ones, then those of the highest score, equal ones by the lower number,
+ *   score = sum over the group's tokens and the KV head's query heads of
+ *           sum_e max(q_e hi_e, q_e lo_e),
+ * hi and lo the block's bounds: scale * score is at least the sum of the queries' logits with any
+ * row of the block.  Formed in binary64; NaN ranks below every number.
+ *   q     [N][n_q_heads][head_dim], dtype, contiguous: normed and rotated as the keys are
+ *   list  written: the chosen blocks ascending, -1 behind them (and for groups without tokens)
+ * Workspace: dc_block_workspace_bytes(dims, tokens, blocks, pick, kv->len + max_tokens), as above.
+ * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_VALUE (first, last), DC_ERR_WORKSPACE, DC_ERR_UNSUPPORTED (rows, count,
+ * alignment, more than 16384 blocks of a unit, grids). */
+dc_status dc_block_select(const dc_dims *dims, const dc_kv *kv, int32_t layer, const dc_tokens *tokens,
+                          const dc_blocks *blocks, const dc_pick *pick, const void *q, int32_t *list, void *ws,
+                          size_t ws_bytes, void *hip_stream);
+
+/* Causal attention as dc_prompt_attention's over part of the rows: a token sees the rows of the blocks
+ * that its group's list names, the rows behind the unit's last complete block, and its
+ * sequence's tokens up to itself.
+ *   list   as dc_block_select leaves it, or the caller's own (one layer's choice serves others): of its entries
+ *          those count that name a complete block and are above all such entries before them, so
+ *          that no block counts twice.  pick->count and share say its layout; blocks->bounds is not read.
+ * Workspace: as dc_block_select.
+ * Errors: those of dc_prompt_attention; DC_ERR_NULL (blocks, pick, list), DC_ERR_UNSUPPORTED and DC_ERR_VALUE
+ * as dc_block_select. */
+dc_status dc_block_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer, const dc_tokens *tokens,
+                             const dc_blocks *blocks, const dc_pick *pick, const int32_t *list, const void *q,
+                             void *out, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Workspace bytes of dc_block_select and dc_block_attention for caches of up to max_len rows, the tokens' own
+ * included (>= max_tokens).  0 also for invalid sizes. */
+size_t dc_block_workspace_bytes(const dc_dims *dims, const dc_tokens *tokens, const dc_blocks *blocks,
+                                const dc_pick *pick, int32_t max_len);
+
 /* Static string naming a status. */
 const char *dc_status_str(dc_status s);
 

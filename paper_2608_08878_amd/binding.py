@@ -70,7 +70,22 @@ class dc_rope(ctypes.Structure):
                 ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p)]
 
 
+class dc_shared(ctypes.Structure):
+    _fields_ = [("kv", ctypes.POINTER(dc_kv)), ("capacity", ctypes.c_int32), ("prefixes", ctypes.c_int32),
+                ("max_members", ctypes.c_int32), ("first", ctypes.c_void_p)]
+
+
+class dc_blocks(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("bounds", ctypes.c_void_p)]
+
+
+class dc_pick(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("share", ctypes.c_int32), ("first", ctypes.c_int32),
+                ("last", ctypes.c_int32)]
+
+
 TREE_MAX_NODES = 256
+MAX_CHOSEN = 2048
 KL_MAX_ROWS = 16384
 KL_STATIC_MAX_PAIRS = 524288     # rows * (vocab / 64) of one dc_kl_reward_static call
 
@@ -83,7 +98,8 @@ EXPORTS = ("dc_workspace_bytes", "dc_feat_init", "dc_decode_step", "dc_score_evi
            "dc_reinforce_terms",
            "dc_dynamic_budget", "dc_global_alpha", "dc_global_alpha_workspace_bytes",
            "dc_qk_norm_rope", "dc_prompt_attention", "dc_tree_attention", "dc_commit_rows",
-           "dc_tokens_workspace_bytes", "dc_status_str")
+           "dc_tokens_workspace_bytes", "dc_shared_attention", "dc_shared_workspace_bytes", "dc_block_bounds",
+           "dc_block_select", "dc_block_attention", "dc_block_workspace_bytes", "dc_status_str")
 
 _lib = None
 
@@ -169,6 +185,20 @@ def lib() -> ctypes.CDLL:
         L.dc_commit_rows.restype = ctypes.c_int
         L.dc_tokens_workspace_bytes.argtypes = [ctypes.POINTER(dc_dims), ctypes.POINTER(dc_tokens), i32]
         L.dc_tokens_workspace_bytes.restype = sz
+        dims, kv, tok = ctypes.POINTER(dc_dims), ctypes.POINTER(dc_kv), ctypes.POINTER(dc_tokens)
+        blocks, pick, shared = ctypes.POINTER(dc_blocks), ctypes.POINTER(dc_pick), ctypes.POINTER(dc_shared)
+        L.dc_shared_attention.argtypes = [dims, kv, i32, tok, vp, shared, vp, vp, vp, sz, vp]
+        L.dc_shared_attention.restype = ctypes.c_int
+        L.dc_shared_workspace_bytes.argtypes = [dims, tok, shared, i32]
+        L.dc_shared_workspace_bytes.restype = sz
+        L.dc_block_bounds.argtypes = [dims, kv, blocks, i32, vp]
+        L.dc_block_bounds.restype = ctypes.c_int
+        L.dc_block_select.argtypes = [dims, kv, i32, tok, blocks, pick, vp, vp, vp, sz, vp]
+        L.dc_block_select.restype = ctypes.c_int
+        L.dc_block_attention.argtypes = [dims, kv, i32, tok, blocks, pick, vp, vp, vp, vp, sz, vp]
+        L.dc_block_attention.restype = ctypes.c_int
+        L.dc_block_workspace_bytes.argtypes = [dims, tok, blocks, pick, i32]
+        L.dc_block_workspace_bytes.restype = sz
         L.dc_status_str.argtypes = [ctypes.c_int]
         L.dc_status_str.restype = ctypes.c_char_p
         _lib = L
@@ -344,3 +374,37 @@ def dc_tokens_workspace_bytes(dims, tokens, max_len: int) -> int:
 def dc_commit_rows(dims, kv, feat, tokens, path=None, keep=None, width: int = 0, stream=None) -> None:
     _check(lib().dc_commit_rows(ctypes.byref(dims), ctypes.byref(kv), _ref(feat), ctypes.byref(tokens),
                                 _ptr(path), _ptr(keep), width, stream))
+
+
+def dc_shared_attention(dims, kv, layer: int, tokens, parent, shared, q, out, ws=None, ws_bytes: int = 0,
+                        stream=None) -> None:
+    _check(lib().dc_shared_attention(ctypes.byref(dims), ctypes.byref(kv), layer, ctypes.byref(tokens), _ptr(parent),
+                                     ctypes.byref(shared), _ptr(q), _ptr(out), _ptr(ws), ws_bytes, stream))
+
+
+def dc_shared_workspace_bytes(dims, tokens, shared, max_len: int) -> int:
+    return int(lib().dc_shared_workspace_bytes(ctypes.byref(dims), ctypes.byref(tokens), ctypes.byref(shared),
+                                               max_len))
+
+
+def dc_block_bounds(dims, kv, blocks, start: int = 0, stream=None) -> None:
+    _check(lib().dc_block_bounds(ctypes.byref(dims), ctypes.byref(kv), ctypes.byref(blocks), start, stream))
+
+
+def dc_block_select(dims, kv, layer: int, tokens, blocks, pick, q, list_out, ws=None, ws_bytes: int = 0,
+                    stream=None) -> None:
+    _check(lib().dc_block_select(ctypes.byref(dims), ctypes.byref(kv), layer, ctypes.byref(tokens),
+                                 ctypes.byref(blocks), ctypes.byref(pick), _ptr(q), _ptr(list_out), _ptr(ws), ws_bytes,
+                                 stream))
+
+
+def dc_block_attention(dims, kv, layer: int, tokens, blocks, pick, chosen, q, out, ws=None, ws_bytes: int = 0,
+                       stream=None) -> None:
+    _check(lib().dc_block_attention(ctypes.byref(dims), ctypes.byref(kv), layer, ctypes.byref(tokens),
+                                    ctypes.byref(blocks), ctypes.byref(pick), _ptr(chosen), _ptr(q), _ptr(out),
+                                    _ptr(ws), ws_bytes, stream))
+
+
+def dc_block_workspace_bytes(dims, tokens, blocks, pick, max_len: int) -> int:
+    return int(lib().dc_block_workspace_bytes(ctypes.byref(dims), ctypes.byref(tokens), ctypes.byref(blocks),
+                                              ctypes.byref(pick), max_len))

@@ -339,6 +339,126 @@ class DecodeBuffers:
         q, _ = self.norm_rope(tokens, rope, q, k, v, pos, layer, stream=stream)
         return self.tree_attention(tokens, parent, q, layer, out, stream)
 
+    # ---- rows that sequences share, and blocks of rows
+
+    def reserve_shared_workspace(self, tokens, shared, max_len: int, stream=None):
+        """As reserve_tokens_workspace, for shared_attention with prefixes of their present lengths."""
+        self._grow(B.dc_shared_workspace_bytes(self.dims, tokens, shared, max_len), stream)
+
+    def shared_attention(self, tokens, shared, q, parent=None, layer=0, out=None, stream=None):
+        """prompt_attention (or with `parent` tree_attention) of sequences whose prefixes (make_shared) hold
+        rows that they have in common; those are read once for all of them."""
+        out = self._check_queries(tokens, q, out, stream)
+        if shared.like != self._like_heads() or shared.device != self._device:
+            raise ValueError("the prefixes must have the cache's layers, heads, head_dim, dtype and device")
+        if shared.sequences > self.dims.batch:
+            raise ValueError(f"prefixes of {shared.sequences} sequences for a cache of {self.dims.batch}")
+        if parent is not None:
+            self._ints(parent, (tokens.tokens,), "parent")
+        shared.update()
+        self.reserve_shared_workspace(tokens, shared, self.kv.len + tokens.max_tokens, stream)
+        B.dc_shared_attention(self.dims, self.kv, layer, tokens, parent, shared, q, out, self.ws, self.ws_bytes,
+                              self._stream_here(stream))
+        return out
+
+    def _like_heads(self):
+        d = self.dims
+        return d.n_layers, d.n_q_heads, d.n_kv_heads, d.head_dim, d.dtype
+
+    def make_blocks(self, rows=64) -> B.dc_blocks:
+        """Blocks of `rows` rows of this cache, their bounds all zero (block_bounds computes them)."""
+        if rows not in (16, 32, 64, 128):
+            raise ValueError(f"blocks of {rows} rows: must be 16, 32, 64 or 128")
+        x = torch.zeros((self.U, self.cap // rows, 2, self.D), dtype=self.k.dtype, device=self.k.device)
+        b = B.dc_blocks(rows, x.data_ptr() or None)
+        b.bounds_tensor = x                          # kept alive with b
+        return b
+
+    def _blocks_of(self, blocks):
+        x = blocks.bounds_tensor
+        if x.shape != (self.U, self.cap // blocks.rows, 2, self.D) or x.dtype != self.k.dtype:
+            raise ValueError("the blocks are those of another cache")
+        self._here(x, "blocks")
+
+    def block_bounds(self, blocks, start=0, stream=None):
+        """The bounds of all complete blocks that hold a row from `start` on, every layer's: `start` is the rows
+        that every unit had at the last call, or 0 after an eviction."""
+        self._blocks_of(blocks)
+        B.dc_block_bounds(self.dims, self.kv, blocks, start, self._stream_here(stream))
+
+    def reserve_block_workspace(self, tokens, blocks, count, max_len: int, share=1, stream=None):
+        """As reserve_tokens_workspace, for block_select and block_attention."""
+        self._grow(B.dc_block_workspace_bytes(self.dims, tokens, blocks, B.dc_pick(count, share, 0, 0), max_len), stream)
+
+    def _lists(self, tokens, count, share):
+        return self.dims.batch, -(-tokens.max_tokens // share), self.dims.n_kv_heads, count
+
+    def block_select(self, tokens, blocks, q, count, share=1, first=0, last=0, layer=0, out=None, stream=None):
+        """The `count` blocks that every `share` successive tokens read, for each KV head: the first and last ones
+        named so and those whose bound of the queries' logits is the highest.
+        Returns int32 [batch][ceil(max_tokens / share)][n_kv_heads][count], ascending, -1 behind."""
+        self._batch_of(tokens)
+        self._blocks_of(blocks)
+        self._like(q, tokens, self.dims.n_q_heads, "q")
+        if count < 1 or share < 1:
+            raise ValueError("count and share must be at least 1")
+        shape = self._lists(tokens, count, share)
+        if out is not None:
+            self._ints(out, shape, "out")
+        elif stream is None:
+            out = torch.empty(shape, dtype=torch.int32, device=self.k.device)
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty(shape, dtype=torch.int32, device=self.k.device)
+        self.reserve_block_workspace(tokens, blocks, count, self.kv.len + tokens.max_tokens, share, stream)
+        B.dc_block_select(self.dims, self.kv, layer, tokens, blocks, B.dc_pick(count, share, first, last), q, out, self.ws,
+                          self.ws_bytes, self._stream_here(stream))
+        return out
+
+    def block_attention(self, tokens, blocks, chosen, q, share=1, layer=0, out=None, stream=None):
+        """Causal attention over the chosen blocks (block_select's lists, or another choice in that layout), the
+        rows behind the last complete block and the tokens themselves."""
+        out = self._check_queries(tokens, q, out, stream)
+        self._blocks_of(blocks)
+        if share < 1 or chosen.dim() != 4:
+            raise ValueError("share must be at least 1 and chosen [batch][groups][n_kv_heads][count]")
+        count = chosen.shape[3]
+        self._ints(chosen, self._lists(tokens, count, share), "chosen")
+        self.reserve_block_workspace(tokens, blocks, count, self.kv.len + tokens.max_tokens, share, stream)
+        B.dc_block_attention(self.dims, self.kv, layer, tokens, blocks, B.dc_pick(count, share, 0, 0), chosen, q, out,
+                             self.ws, self.ws_bytes, self._stream_here(stream))
+        return out
+
+    def sparse_attention(self, tokens, blocks, q, count, share=1, first=0, last=0, layer=0, out=None, stream=None):
+        """block_select and block_attention of one layer."""
+        chosen = self.block_select(tokens, blocks, q, count, share, first, last, layer, stream=stream)
+        return self.block_attention(tokens, blocks, chosen, q, share, layer, out, stream)
+
+
+def make_shared(prefix: DecodeBuffers, members=None) -> B.dc_shared:
+    """The caches of `prefix` (one sequence each) as rows that sequences of another DecodeBuffers have in common:
+    the first members[0] sequences those of prefix 0, the next members[1] those of prefix 1 and so on,
+    sequences behind them none.  An int: so many each, which are then all sequences."""
+    n = prefix.dims.batch
+    equal = isinstance(members, int)
+    counts = [members] * n if equal else [int(m) for m in members]
+    if len(counts) != n or min(counts) < 0 or max(counts) < 1 or sum(counts) >= 1 << 24:
+        raise ValueError(f"members must be the numbers of sequences of {n} prefixes, at least 0, one of them more")
+    s = B.dc_shared(ctypes.pointer(prefix.kv), prefix.cap, n, max(counts), None)
+    s.prefix = prefix                                # kept alive with s
+    s.like, s.device, s.sequences = prefix._like_heads(), prefix._device, sum(counts)
+    if not equal:
+        first = [0]
+        for m in counts:
+            first.append(first[-1] + m)
+        s.first_tensor = torch.tensor(first, dtype=torch.int32, device=prefix.k.device)
+        s.first = s.first_tensor.data_ptr()
+
+    def update():                                    # (shrink moves the rows to other buffers)
+        s.capacity = prefix.cap
+    s.update = update
+    return s
+
 
 def make_tokens(counts, device="cuda") -> B.dc_tokens:
     """Packed tokens of sequences of `counts` (host) tokens each."""

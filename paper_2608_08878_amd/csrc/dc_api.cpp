@@ -940,6 +940,114 @@ dc_status attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_t
   return dc::launch_attend(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
 }
 
+// What the attentions take beside their key ranges.
+dc_status check_attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens, const void* q,
+                       const void* out) {
+  dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  if (!q || !out) return DC_ERR_NULL;
+  if (layer < 0 || layer >= dims->n_layers) return DC_ERR_SHAPE;
+  st = check_rows(dims, kv, tokens);
+  if (st != DC_OK) return st;
+  if (!aligned16(q) || !aligned16(out)) return DC_ERR_UNSUPPORTED;
+  const int64_t width = (int64_t)dims->n_q_heads * dims->head_dim;
+  return overlap(dims, q, tokens->tokens, width, width, out, tokens->tokens, width, width) ? DC_ERR_UNSUPPORTED : DC_OK;
+}
+
+template <typename Args>
+void fill_attend(const dc_dims* dims, const dc_tokens* t, Args& a) {
+  memset(&a, 0, sizeof(a));
+  a.tok = token_args(t);
+  a.batch = dims->batch;
+  a.n_layers = dims->n_layers;
+  a.hq = dims->n_q_heads;
+  a.hk = dims->n_kv_heads;
+  a.gshift = log2_of(group_of(dims));
+  a.cap = dims->capacity;
+  a.scale = scale_of(dims);
+}
+
+// Bytes of the parts of a call's outputs.
+size_t parts_bytes(const dc_dims* dims, const dc_tokens* t, const dc::AttendArgs& a, int least) {
+  const size_t each = (size_t)t->tokens * dims->n_q_heads * (dims->head_dim + 2) * sizeof(float);
+  return a.most_splits > least ? align256(each * a.most_splits) : 0;
+}
+
+dc_status check_shared(const dc_dims* dims, const dc_shared* s) {
+  if (!s || !s->kv) return DC_ERR_NULL;
+  if (s->prefixes < 1 || s->capacity < 1 || s->max_members < 1 || s->max_members > dims->batch) return DC_ERR_SHAPE;
+  if (s->kv->len < 0 || s->kv->len > s->capacity) return DC_ERR_SHAPE;
+  if (!s->first && (int64_t)s->prefixes * s->max_members != dims->batch) return DC_ERR_SHAPE;
+  if ((int64_t)s->prefixes * dims->n_layers * dims->n_kv_heads > (1 << 24) || s->capacity > (1 << 26))
+    return DC_ERR_UNSUPPORTED;
+  return DC_OK;
+}
+
+bool plan_shared(const dc_dims* dims, const dc_tokens* t, const dc_shared* s, int L, dc::SharedArgs& a, size_t& need) {
+  fill_attend(dims, t, a);
+  a.pcap = s->capacity;
+  a.prefixes = s->prefixes;
+  a.max_members = s->max_members;
+  a.plen = s->kv->len;
+  const int64_t most = (int64_t)s->max_members * t->max_tokens;
+  a.group_tokens = (int)(most < t->tokens ? most : t->tokens);
+  if (!dc::shared_plan(a, dims->dtype, dims->head_dim, L, a.plen > 0 ? a.plen : 1)) return false;
+  need = parts_bytes(dims, t, a, 0);
+  return true;
+}
+
+dc_status check_blocks(const dc_dims* dims, const dc_blocks* b, bool bounds) {
+  if (!b) return DC_ERR_NULL;
+  if (b->rows != 16 && b->rows != 32 && b->rows != 64 && b->rows != 128) return DC_ERR_UNSUPPORTED;
+  if (!bounds) return DC_OK;
+  if (!b->bounds && dims->capacity >= b->rows) return DC_ERR_NULL;      // (a cache of less than a block has none)
+  return aligned16(b->bounds) ? DC_OK : DC_ERR_UNSUPPORTED;
+}
+
+int block_shift(int rows) { return rows == 16 ? 4 : rows == 32 ? 5 : rows == 64 ? 6 : 7; }
+
+dc_status check_pick(const dc_pick* p) {
+  if (!p) return DC_ERR_NULL;
+  if (p->count < 1 || p->share < 1) return DC_ERR_SHAPE;
+  if (p->count > DC_MAX_CHOSEN) return DC_ERR_UNSUPPORTED;
+  if (p->first < 0 || p->last < 0 || p->first > p->count || p->last > p->count - p->first) return DC_ERR_VALUE;
+  return DC_OK;
+}
+
+int groups_of(const dc_tokens* t, int share) { return (int)(((int64_t)t->max_tokens + share - 1) / share); }
+
+bool plan_blocks(const dc_dims* dims, const dc_tokens* t, const dc_blocks* b, const dc_pick* p, int L, dc::BlockArgs& a,
+                 size_t& need) {
+  fill_attend(dims, t, a);
+  a.count = p->count;
+  a.bshift = block_shift(b->rows);
+  a.share = p->share;
+  a.groups = groups_of(t, p->share);
+  if (!dc::block_plan(a, dims->dtype, dims->head_dim, L)) return false;
+  need = parts_bytes(dims, t, a, 1);
+  return true;
+}
+
+bool plan_select(const dc_dims* dims, const dc_tokens* t, const dc_blocks* b, const dc_pick* p, int len,
+                 dc::SelectArgs& a, size_t& need) {
+  memset(&a, 0, sizeof(a));
+  a.tok = token_args(t);
+  a.batch = dims->batch;
+  a.n_layers = dims->n_layers;
+  a.hq = dims->n_q_heads;
+  a.hk = dims->n_kv_heads;
+  a.gshift = log2_of(group_of(dims));
+  a.cap = dims->capacity;
+  a.len = len;
+  a.bshift = block_shift(b->rows);
+  a.share = p->share;
+  a.groups = groups_of(t, p->share);
+  a.count = p->count;
+  a.first = p->first;
+  a.last = p->last;
+  return dc::select_fits(a, need);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1091,6 +1199,138 @@ dc_status dc_commit_rows(const dc_dims* dims, dc_kv* kv, dc_feat* feat, const dc
   kv->len += width;
   if (feat) advance_pos(feat, width, row);
   return DC_OK;
+}
+
+size_t dc_shared_workspace_bytes(const dc_dims* dims, const dc_tokens* tokens, const dc_shared* shared,
+                                 int32_t max_len) {
+  if (check_tokens(dims, tokens) != DC_OK || check_shared(dims, shared) != DC_OK || max_len < 1) return 0;
+  dc::SharedArgs a;
+  size_t need = 0;
+  if (!plan_shared(dims, tokens, shared, max_len, a, need)) return 0;
+  const size_t alone = dc_tokens_workspace_bytes(dims, tokens, max_len);     // (prefixes without rows)
+  return need > alone ? need : alone;
+}
+
+dc_status dc_shared_attention(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens,
+                              const int32_t* parent, const dc_shared* shared, const void* q, void* out, void* ws,
+                              size_t ws_bytes, void* hip_stream) {
+  dc_status st = check_attend(dims, kv, layer, tokens, q, out);
+  if (st != DC_OK) return st;
+  st = check_shared(dims, shared);
+  if (st != DC_OK) return st;
+  if (!shared->kv->k || !shared->kv->v) return DC_ERR_NULL;
+  if (!aligned16(shared->kv->k) || !aligned16(shared->kv->v)) return DC_ERR_UNSUPPORTED;
+  if (parent && tokens->max_tokens > DC_TREE_MAX_NODES) return DC_ERR_UNSUPPORTED;
+  if (shared->kv->len == 0) return attend(dims, kv, layer, tokens, parent, q, out, ws, ws_bytes, hip_stream);
+  dc::SharedArgs a;
+  size_t need = 0;
+  if (!plan_shared(dims, tokens, shared, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
+  if (!ws || ws_bytes < need) return DC_ERR_WORKSPACE;
+  if (!aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  a.q = q;
+  a.out = out;
+  a.k = kv->k;
+  a.v = kv->v;
+  a.unit_len = kv->unit_len;
+  a.parent = parent;
+  a.part = (float*)ws;
+  a.layer = layer;
+  a.len = kv->len;
+  a.pk = shared->kv->k;
+  a.pv = shared->kv->v;
+  a.punit_len = shared->kv->unit_len;
+  a.first = shared->first;
+  return dc::launch_shared(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
+}
+
+dc_status dc_block_bounds(const dc_dims* dims, const dc_kv* kv, const dc_blocks* blocks, int32_t from,
+                          void* hip_stream) {
+  dc_status st = check_dims(dims);
+  if (st != DC_OK) return st;
+  if (!kv || !kv->k) return DC_ERR_NULL;
+  if (kv->len < 0 || kv->len > dims->capacity || from < 0 || from > kv->len) return DC_ERR_SHAPE;
+  st = check_blocks(dims, blocks, true);
+  if (st != DC_OK) return st;
+  if (!aligned16(kv->k)) return DC_ERR_UNSUPPORTED;
+  dc::BoundsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.k = kv->k;
+  a.bounds = blocks->bounds;
+  a.unit_len = kv->unit_len;
+  a.cap = dims->capacity;
+  a.units = (int)units_of(dims);
+  a.len = kv->len;
+  a.from = from;
+  a.bshift = block_shift(blocks->rows);
+  return dc::launch_bounds(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
+}
+
+size_t dc_block_workspace_bytes(const dc_dims* dims, const dc_tokens* tokens, const dc_blocks* blocks,
+                                const dc_pick* pick, int32_t max_len) {
+  if (check_tokens(dims, tokens) != DC_OK || check_blocks(dims, blocks, false) != DC_OK || check_pick(pick) != DC_OK ||
+      max_len < tokens->max_tokens)
+    return 0;
+  dc::BlockArgs a;
+  dc::SelectArgs c;
+  size_t need = 0, keys = 0;
+  if (!plan_blocks(dims, tokens, blocks, pick, max_len, a, need)) return 0;
+  if (!plan_select(dims, tokens, blocks, pick, max_len - tokens->max_tokens, c, keys)) keys = 0;   // (refused)
+  return need > keys ? need : keys;
+}
+
+dc_status dc_block_select(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens,
+                          const dc_blocks* blocks, const dc_pick* pick, const void* q, int32_t* list, void* ws,
+                          size_t ws_bytes, void* hip_stream) {
+  dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  if (!q || !list || !kv) return DC_ERR_NULL;
+  if (layer < 0 || layer >= dims->n_layers) return DC_ERR_SHAPE;
+  if (kv->len < 0 || kv->len > dims->capacity) return DC_ERR_SHAPE;
+  st = check_blocks(dims, blocks, true);
+  if (st != DC_OK) return st;
+  st = check_pick(pick);
+  if (st != DC_OK) return st;
+  if (!aligned16(q) || ((uintptr_t)list & 3)) return DC_ERR_UNSUPPORTED;
+  dc::SelectArgs a;
+  size_t need = 0;
+  if (!plan_select(dims, tokens, blocks, pick, kv->len, a, need)) return DC_ERR_UNSUPPORTED;
+  if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
+  if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  a.q = q;
+  a.bounds = blocks->bounds;
+  a.unit_len = kv->unit_len;
+  a.list = list;
+  a.keys = need ? (uint64_t*)ws : nullptr;
+  a.layer = layer;
+  return dc::launch_select(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
+}
+
+dc_status dc_block_attention(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens,
+                             const dc_blocks* blocks, const dc_pick* pick, const int32_t* list, const void* q,
+                             void* out, void* ws, size_t ws_bytes, void* hip_stream) {
+  dc_status st = check_attend(dims, kv, layer, tokens, q, out);
+  if (st != DC_OK) return st;
+  if (!list) return DC_ERR_NULL;
+  st = check_blocks(dims, blocks, false);
+  if (st != DC_OK) return st;
+  st = check_pick(pick);
+  if (st != DC_OK) return st;
+  if ((uintptr_t)list & 3) return DC_ERR_UNSUPPORTED;
+  dc::BlockArgs a;
+  size_t need = 0;
+  if (!plan_blocks(dims, tokens, blocks, pick, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
+  if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
+  if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  a.q = q;
+  a.out = out;
+  a.k = kv->k;
+  a.v = kv->v;
+  a.unit_len = kv->unit_len;
+  a.list = list;
+  a.part = need ? (float*)ws : nullptr;
+  a.layer = layer;
+  a.len = kv->len;
+  return dc::launch_blocks(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
 }
 
 }  // extern "C"

@@ -197,6 +197,53 @@ struct AttendArgs {
   int once;                 // 1: K/V rows are read once, by non-temporal loads
 };
 
+// The same of sequences that have rows in common (dc_shared.hip).  A row of `part` holds the parts of the
+// shared rows, psplits of them, then those of the sequence's own: splits in all.
+struct SharedArgs : AttendArgs {
+  const void* pk;           // [prefix units][pcap][D]
+  const void* pv;
+  const int32_t* punit_len; // [prefix units] or null: plen each
+  const int32_t* first;     // [prefixes + 1] first sequence of every prefix, or null: max_members each
+  int64_t pcap;
+  int prefixes, max_members, plen;
+  int group_tokens;         // bound of the tokens of one prefix's sequences
+  int psplits, pchunk;      // parts of the shared rows, pchunk each
+  int shared_wgs;           // workgroups of the shared rows, which come first
+};
+
+// The same over chosen blocks of the rows (dc_blocks.hip).
+struct BlockArgs : AttendArgs {
+  const int32_t* list;      // [batch][groups][hk][count] blocks
+  int count;
+  int bshift;               // log2 of a block's rows
+  int share, groups;        // tokens of a list, lists of a sequence and KV head
+  int group_tiles;          // row tiles of a list
+};
+
+// Bounds of the keys of blocks, and the choice of blocks by them (dc_blocks.hip).
+struct BoundsArgs {
+  const void* k;            // [units][cap][D]
+  void* bounds;             // [units][cap / rows][2][D] largest and smallest elements
+  const int32_t* unit_len;
+  int64_t cap;
+  int units, len, from;
+  int bshift;
+  int y0;                   // first grid row of the launch (see for_grid_y)
+};
+
+struct SelectArgs {
+  const void* q;            // [N][hq][D]
+  const void* bounds;
+  const int32_t* unit_len;
+  int32_t* list;            // [batch][groups][hk][count]
+  uint64_t* keys;           // [lists][ld_keys] ranks of the blocks
+  int64_t cap;
+  TokenArgs tok;
+  int batch, n_layers, layer, hq, hk, gshift, len, bshift;
+  int share, groups, count, first, last;
+  int ld_keys;
+};
+
 // The rows behind each unit's length become part of the cache (dc_rows.hip).
 struct CommitArgs {
   void* k;
@@ -276,5 +323,14 @@ int launch_commit(const CommitArgs& a, int dtype, int D, void* stream);
 // rows, the tokens' own included; returns false when its grid is out of range.
 bool attend_plan(AttendArgs& a, int dtype, int D, int L);
 int launch_attend(const AttendArgs& a, int dtype, int D, void* stream);
+// The same for shared rows (of up to Lp) and chosen blocks.
+bool shared_plan(SharedArgs& a, int dtype, int D, int L, int Lp);
+int launch_shared(const SharedArgs& a, int dtype, int D, void* stream);
+bool block_plan(BlockArgs& a, int dtype, int D, int L);
+int launch_blocks(const BlockArgs& a, int dtype, int D, void* stream);
+int launch_bounds(const BoundsArgs& a, int dtype, int D, void* stream);
+// Whether the launcher takes such a choice, and bytes of `keys`.
+bool select_fits(const SelectArgs& a, size_t& key_bytes);
+int launch_select(const SelectArgs& a, int dtype, int D, void* stream);
 
 }  // namespace dc
