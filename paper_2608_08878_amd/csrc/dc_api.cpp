@@ -1045,7 +1045,7 @@ bool plan_select(const dc_dims* dims, const dc_tokens* t, const dc_blocks* b, co
   a.count = p->count;
   a.first = p->first;
   a.last = p->last;
-  return dc::select_fits(a, need);
+  return dc::select_plan(a, need);
 }
 
 }  // namespace

@@ -790,8 +790,22 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
 
 // Joins the parts of the key range, a wave per row: lane x holds part x's maximum and sum, then the
 // wave adds the parts' outputs, eight loads under way.
-template <int DT, int D, int MODE>
-__global__ void __launch_bounds__(256) attend_join_kernel(ArgsOf<MODE> a) {
+template <int DT, int D>
+__device__ __forceinline__ void store_joined(const AttendArgs& a, size_t qrow, const float* o, float l, int lane) {
+  constexpr int EPL = D / 64;
+  const float inv = 1.0f / l;
+  const size_t at = qrow * D + lane * EPL;
+  if constexpr (DT == 1 && EPL == 2)
+    reinterpret_cast<uint32_t*>(a.out)[at / 2] = pack_bf16(o[0] * inv, o[1] * inv);
+  else if constexpr (DT == 1)
+    reinterpret_cast<uint16_t*>(a.out)[at] = (uint16_t)f32_to_bf16_bits(o[0] * inv);
+  else
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) reinterpret_cast<float*>(a.out)[at + e] = o[e] * inv;
+}
+
+template <int DT, int D>
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   constexpr int EPL = D / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pairs = a.batch * a.hk;
@@ -802,20 +816,69 @@ __global__ void __launch_bounds__(256) attend_join_kernel(ArgsOf<MODE> a) {
   token_range(a.tok, b, t0, n);
   if (row >= n << a.gshift) return;
   const int r = row >> a.gshift, head = (g << a.gshift) + (row & ((1 << a.gshift) - 1));
+  const int keys = rows_before(a.unit_len, a.len, u) + (a.parent ? n : r + 1);
+  const int parts = (keys + a.chunk - 1) / a.chunk;       // those that a kernel wrote: at most MAX_PARTS
   const size_t qrow = (size_t)(t0 + r) * a.hq + head;
   const float* po = a.part + qrow * a.splits * D + lane * EPL;
   const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D) +
                      qrow * a.splits;
-  // those that a kernel wrote, at most MAX_PARTS: 0 .. common - 1, and behind psplits the own rows'
-  int parts, common = 0, gap = 0;
-  if constexpr (MODE == BLOCKS) {
-    parts = a.splits;
-  } else {
-    const int keys = rows_before(a.unit_len, a.len, u) + (a.parent ? n : r + 1);
-    parts = (keys + a.chunk - 1) / a.chunk;
+  const float2 mine = lane < parts ? ml[lane] : make_float2(NEG_INF, 0.0f);
+  float m = mine.x;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  const float f = lane < parts ? rescale(mine.x, m) : 0.0f;
+  float l = mine.y * f, o[EPL] = {};
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
+  for (int s = 0; s < parts; s += 8) {
+    float v[8][EPL];
+#pragma unroll
+    for (int y = 0; y < 8; ++y)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) v[y][e] = s + y < parts ? po[(size_t)(s + y) * D + e] : 0.0f;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const float fy = __shfl(f, s + y);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(v[y][e], fy, o[e]);
+    }
   }
-  if constexpr (is_shared(MODE)) {
-    int p = b / a.max_members;
+  store_joined<DT, D>(a, qrow, o, l, lane);
+}
+
+// The same of shared rows or chosen blocks, whose parts are not all there: lane x holds place x's maximum and sum.
+// The first places' outputs are under way while the lengths say which hold a part (loads of the others are
+// of memory that is the call's, and dropped).
+template <int DT, int D, int MODE>
+__global__ void __launch_bounds__(256) places_join_kernel(ArgsOf<MODE> a) {
+  constexpr int EPL = D / 64, N = 16;
+  typedef float vec_t __attribute__((ext_vector_type(EPL)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pairs = a.batch * a.hk;
+  const int pair = blockIdx.x % pairs, row = (blockIdx.x / pairs) * 4 + wave;
+  const int b = pair / a.hk, g = pair % a.hk;
+  int t0, n;
+  token_range(a.tok, b, t0, n);
+  if (row >= n << a.gshift) return;
+  const int r = row >> a.gshift, head = (g << a.gshift) + (row & ((1 << a.gshift) - 1));
+  const size_t qrow = (size_t)(t0 + r) * a.hq + head;
+  const vec_t* po = reinterpret_cast<const vec_t*>(a.part + qrow * a.splits * D) + lane;
+  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D) +
+                     qrow * a.splits;
+  float2 mine = ml[lane < a.splits ? lane : 0];
+  vec_t v[N];
+  auto load = [&](int s) DC_INLINE {
+#pragma unroll
+    for (int y = 0; y < N; ++y) v[y] = po[(size_t)(s + y < a.splits ? s + y : 0) * (D / EPL)];
+  };
+  load(0);
+  bool live = lane < a.splits;
+  if constexpr (MODE == BLOCKS) {
+    live = live && mine.y != NO_PART;
+  } else {
+    const int u = (b * a.n_layers + a.layer) * a.hk + g;
+    const int keys = rows_before(a.unit_len, a.len, u) + (a.parent ? n : r + 1);
+    int p = b / a.max_members, common = 0;
     if (a.first) {                        // the last prefix that begins at or before sequence b
       p = 0;
       for (int p0 = 1; p0 < a.prefixes; p0 += 64) {
@@ -831,46 +894,32 @@ __global__ void __launch_bounds__(256) attend_join_kernel(ArgsOf<MODE> a) {
       if (b >= f0 && b < f1 && t0 + r >= s0 && t0 + r < s0 + sn)
         common = (rows_before(a.punit_len, a.plen, (p * a.n_layers + a.layer) * a.hk + g) + a.pchunk - 1) / a.pchunk;
     }
-    common = __builtin_amdgcn_readfirstlane(common);
-    parts += common;
-    gap = a.psplits - common;
+    live = live && (lane < a.psplits ? lane < common : lane - a.psplits < (keys + a.chunk - 1) / a.chunk);
   }
-  const int slot = is_shared(MODE) && lane >= common ? lane + gap : lane;
-  float2 mine = lane < parts ? ml[slot] : make_float2(NEG_INF, 0.0f);
-  const bool none = MODE == BLOCKS && mine.y == NO_PART;
-  if (none) mine = make_float2(NEG_INF, 0.0f);
-  if constexpr (MODE == BLOCKS) parts = 64 - __clzll(__ballot(lane < parts && !none));
+  if (!live) mine = make_float2(NEG_INF, 0.0f);
+  const uint64_t there = __ballot(live);
   float m = mine.x;
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-  const float f = lane < parts ? rescale(mine.x, m) : 0.0f;
-  float l = mine.y * f, o[EPL] = {};
+  const float f = live ? rescale(mine.x, m) : 0.0f;
+  float l = mine.y * f;
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
-  for (int s = 0; s < parts; s += 8) {
-    float v[8][EPL];
+  vec_t o = {};
+  for (int s = 0; s < a.splits; s += N) {
+    if (s > 0) load(s);
 #pragma unroll
-    for (int y = 0; y < 8; ++y) {
-      const int at = is_shared(MODE) && s + y >= common ? s + y + gap : s + y;
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) v[y][e] = s + y < parts ? po[(size_t)at * D + e] : 0.0f;
-    }
-#pragma unroll
-    for (int y = 0; y < 8; ++y) {
-      const float fy = __shfl(f, s + y);
+    for (int y = 0; y < N; ++y) {
+      if (s + y >= 64 || !((there >> (s + y)) & 1)) continue;
+      const float fy = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s + y));
 #pragma unroll
       for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(v[y][e], fy, o[e]);
     }
   }
-  const float inv = 1.0f / l;
-  const size_t at = qrow * D + lane * EPL;
-  if constexpr (DT == 1 && EPL == 2)
-    reinterpret_cast<uint32_t*>(a.out)[at / 2] = pack_bf16(o[0] * inv, o[1] * inv);
-  else if constexpr (DT == 1)
-    reinterpret_cast<uint16_t*>(a.out)[at] = (uint16_t)f32_to_bf16_bits(o[0] * inv);
-  else
+  float out[EPL];
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) reinterpret_cast<float*>(a.out)[at + e] = o[e] * inv;
+  for (int e = 0; e < EPL; ++e) out[e] = o[e];
+  store_joined<DT, D>(a, qrow, out, l, lane);
 }
 
 constexpr int CUS = 256;
@@ -902,8 +951,9 @@ int launch_tiles(const ArgsOf<MODE>& a, int64_t wgs, hipStream_t s) {
 template <int DT, int D, int MODE>
 int launch_join(const ArgsOf<MODE>& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.tok.max_tokens << a.gshift;
-  hipLaunchKernelGGL((attend_join_kernel<DT, D, MODE>), dim3((unsigned)(a.batch * a.hk * ((rows + 3) / 4))), dim3(256),
-                     0, s, a);
+  const dim3 grid((unsigned)(a.batch * a.hk * ((rows + 3) / 4)));
+  if constexpr (MODE > TREE) hipLaunchKernelGGL((places_join_kernel<DT, D, MODE>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_join_kernel<DT, D>), grid, dim3(256), 0, s, a);
   return (int)hipGetLastError();
 }
 

@@ -142,9 +142,10 @@ int bounds_type(const BoundsArgs& a, hipStream_t s) {
 
 // ------------------------------------------------------------------------ choice
 
-constexpr int ST = 512;                  // threads of a workgroup
+constexpr int ST = 256;                  // threads of a workgroup
 constexpr int SW = ST / 64;
-constexpr int MAX_BLOCKS = 16384;        // of a unit: their ranks fill the LDS
+constexpr int MAX_BLOCKS = 16384;        // of a unit: their ranks fill a workgroup's registers
+constexpr int QG = 8, QN = 8;            // lane groups that sum the queries, and loads of each under way
 
 // Scores as integers of the same order: NaN below every number, -0 equal to +0.
 __device__ __forceinline__ uint64_t rank_of(double x) {
@@ -158,62 +159,115 @@ __device__ __forceinline__ double shfl_xor_f64(double x, int mask) {
   return __hiloint2double(hi, lo);
 }
 
-// A sum over the workgroup, for all (two cells of LDS in turn).
-__device__ __forceinline__ int count_all(int x, int* cell) {      // x uniform over a wave
-  if ((threadIdx.x & 63) == 0) cell[threadIdx.x >> 6] = x;
-  __syncthreads();
-  int n = 0;
-#pragma unroll
-  for (int w = 0; w < SW; ++w) n += cell[w];
-  return n;
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double x) {
+  const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, 0xF, 0xF, true);
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, 0xF, 0xF, true), lo);
 }
 
-// One workgroup per list.  The scores are binary64: products of bf16 elements are exact there and sums all
-// but exact, so that a choice next to its limit does not hang on the order of a sum.
-template <int DT, int D>
-__global__ void __launch_bounds__(ST) select_kernel(SelectArgs a) {
-  using R = RowT<DT, D>;
-  constexpr int LPR = R::LPR, EPL = R::EPL, LPB = 2 * LPR, GROUPS = ST / LPR, BPL = 64 / LPB;
-  constexpr int UN = 8;                       // loads of a lane under way
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  __shared__ double qs[2 * D];
-  __shared__ int cells[2][SW];
-  __shared__ uint64_t ends[2][SW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int pairs = a.batch * a.hk, pair = blockIdx.x % pairs, group = blockIdx.x / pairs;
-  const int b = pair / a.hk, g = pair % a.hk, u = (b * a.n_layers + a.layer) * a.hk + g;
-  int t0, n;
-  token_range(a.tok, b, t0, n);
-  int32_t* list = a.list + ((size_t)(b * a.groups + group) * a.hk + g) * a.count;
-  const int r0 = group * a.share, r1 = r0 + a.share < n ? r0 + a.share : n;
-  const int cand = r0 < n ? rows_before(a.unit_len, a.len, u) >> a.bshift : 0;
-  if (cand <= a.count) {                      // all of them, or a group without tokens
-    for (int i = tid; i < a.count; i += ST) list[i] = i < cand ? i : -1;
-    return;
+// Of 2 N numbers the sums with the partner lane's of N: the upper ones where `upper`, as it is not there.
+template <int CTRL, int N>
+__device__ __forceinline__ void fold(double* s, bool upper) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const double give = upper ? s[i] : s[i + N], keep = upper ? s[i + N] : s[i];
+    s[i] = keep + dpp_f64<CTRL>(give);
   }
-  // sums of the queries' positive and negative elements: a lane group a row, the groups in turn
-  const int rows = (r1 - r0) << a.gshift, used = rows < GROUPS ? rows : GROUPS;
-  double* part = reinterpret_cast<double*>(lds);            // [used][2][D]
-  {
-    const int c = tid % LPR, at = tid / LPR;
-    double up[EPL] = {}, down[EPL] = {};
-    for (int i = at; i < rows; i += GROUPS) {
-      const size_t row = (size_t)(t0 + r0 + (i >> a.gshift)) * a.hq + (g << a.gshift) + (i & ((1 << a.gshift) - 1));
-      float f[EPL];
-      unpack_slice<DT>(ldg16((const char*)a.q + row * (D * R::ELT) + c * 16), f);
+}
+
+// Where a list is, and its candidates.
+struct Choice {
+  int b, g, u, t0, r0, r1, cand;
+  int32_t* list;
+};
+__device__ __forceinline__ Choice choice_of(const SelectArgs& a, int index) {
+  Choice c;
+  const int pairs = a.batch * a.hk, pair = index % pairs, group = index / pairs;
+  int n;
+  c.b = pair / a.hk;
+  c.g = pair % a.hk;
+  c.u = (c.b * a.n_layers + a.layer) * a.hk + c.g;
+  token_range(a.tok, c.b, c.t0, n);
+  c.r0 = group * a.share;
+  c.r1 = c.r0 + a.share < n ? c.r0 + a.share : n;
+  c.cand = c.r0 < n ? 1 : 0;               // (candidates_of counts them)
+  c.list = a.list + ((size_t)(c.b * a.groups + group) * a.hk + c.g) * a.count;
+  return c;
+}
+
+__device__ __forceinline__ void candidates_of(const SelectArgs& a, Choice& c) {
+  if (c.cand) c.cand = __builtin_amdgcn_readfirstlane(rows_before(a.unit_len, a.len, c.u) >> a.bshift);
+}
+
+// Ranks of the blocks j0 .. j0 + chunk - 1 to keys[j], if there are such and a choice is to be made.  The scores are binary64: products of bf16 elements are exact there
+// and sums all but exact, so that a choice next to its limit does not hang on the order of a sum.
+template <int DT, int D>
+__device__ __forceinline__ bool score_blocks(const SelectArgs& a, Choice& w, int j0, int chunk, double* part,
+                                             uint64_t* keys) {
+  using R = RowT<DT, D>;
+  constexpr int LPR = R::LPR, EPL = R::EPL, LPB = 2 * LPR, BPL = 64 / LPB;
+  constexpr int UN = 8, STEP = UN * BPL;      // loads of a lane at a time, and the blocks of a wave's
+  __shared__ double qs[2 * D];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // LPB lanes a block, 16 bytes each; the first ones are under way while the queries are summed
+  const int c = lane % LPB;
+  const char* bounds = (const char*)a.bounds + (size_t)w.u * (a.cap >> a.bshift) * (2 * D * R::ELT) + c * 16;
+  uint4 x[UN];
+  auto load = [&](int j, int end) DC_INLINE {
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) {
-        // (NaN stays one in both)
-        up[e] += f[e] < 0.0f ? 0.0 : (double)f[e];
-        down[e] += f[e] > 0.0f ? 0.0 : (double)f[e];
-      }
+    for (int i = 0; i < UN; ++i) {
+      const int at = j + i * BPL + lane / LPB;
+      x[i] = ldg16(bounds + (size_t)(at < end ? at : end - 1) * (2 * D * R::ELT));
     }
-    if (at < used)
+  };
+  // sums of the queries' positive and negative elements: a lane group a row, QG of them in turn, QN rows under way
+  const int rows = (w.r1 - w.r0) << a.gshift, used = rows < QG ? rows : QG;
+  const int qc = tid % LPR, qg = tid / LPR;
+  uint4 qr[QN];
+  auto load_rows = [&](int i0) DC_INLINE {
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) {
-        part[(at * 2) * D + c * EPL + e] = up[e];
-        part[(at * 2 + 1) * D + c * EPL + e] = down[e];
+    for (int x = 0; x < QN; ++x) {
+      int i = i0 + x * QG;
+      i = i < rows ? i : rows - 1;
+      const size_t row = (size_t)(w.t0 + w.r0 + (i >> a.gshift)) * a.hq + (w.g << a.gshift) + (i & ((1 << a.gshift) - 1));
+      qr[x] = ldg16((const char*)a.q + row * (D * R::ELT) + qc * 16);
+    }
+  };
+  static_assert(ST / LPR >= QG, "a lane group for each");
+  const int bound = a.len >> a.bshift;
+  int j = j0 + wave * STEP;
+  if (bound > a.count && w.cand) {
+    if (qg < used) load_rows(qg);
+    load(j, bound);                  // (the unit's own length is still on its way)
+  }
+  candidates_of(a, w);
+  const int j1 = j0 + chunk < w.cand ? j0 + chunk : w.cand;
+  if (w.cand <= a.count || j0 >= j1) return false;
+  if (qg < used) {
+    double up[EPL] = {}, down[EPL] = {};
+    for (int i0 = qg;;) {
+#pragma unroll
+      for (int x = 0; x < QN; ++x) {
+        float f[EPL];
+        unpack_slice<DT>(qr[x], f);
+        if (i0 + x * QG < rows) {
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) {
+            // (NaN stays one in both)
+            up[e] += f[e] < 0.0f ? 0.0 : (double)f[e];
+            down[e] += f[e] > 0.0f ? 0.0 : (double)f[e];
+          }
+        }
       }
+      i0 += QN * QG;
+      if (i0 >= rows) break;
+      load_rows(i0);
+    }
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      part[(qg * 2) * D + qc * EPL + e] = up[e];
+      part[(qg * 2 + 1) * D + qc * EPL + e] = down[e];
+    }
   }
   __syncthreads();
   for (int e = tid; e < 2 * D; e += ST) {
@@ -222,134 +276,261 @@ __global__ void __launch_bounds__(ST) select_kernel(SelectArgs a) {
     qs[e] = s;
   }
   __syncthreads();
-  // scores: LPB lanes a block, 16 bytes each
-  uint64_t* keys = reinterpret_cast<uint64_t*>(lds);
-  const int c = lane % LPB;
   double q[EPL];
 #pragma unroll
   for (int e = 0; e < EPL; ++e) q[e] = qs[c * EPL + e];
-  const char* bounds = (const char*)a.bounds + (size_t)u * (a.cap >> a.bshift) * (2 * D * R::ELT) + c * 16;
-  for (int j0 = wave * UN * BPL; j0 < cand; j0 += SW * UN * BPL) {
-    uint4 w[UN];
+  for (; j < j1; j += SW * STEP) {
     double s[UN];
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
-      const int j = j0 + i * BPL + lane / LPB;
-      w[i] = ldg16(bounds + (size_t)(j < cand ? j : cand - 1) * (2 * D * R::ELT));
-    }
-#pragma unroll
-    for (int i = 0; i < UN; ++i) {
       float f[EPL];
-      unpack_slice<DT>(w[i], f);
+      unpack_slice<DT>(x[i], f);
       s[i] = 0.0;
 #pragma unroll
       for (int e = 0; e < EPL; ++e) s[i] = __builtin_fma((double)f[e], q[e], s[i]);
     }
-    // sums over the block's lanes: three steps that also hand each lane one of the eight
+    load(j + SW * STEP, j1);
+    // sums over the block's lanes: three exchanges in a row of 16 that also leave each lane two of the eight, then
+    // one, and with its neighbour's
+    fold<DPP_MIRROR, 4>(s, lane & 8);
+    fold<DPP_HALF_MIRROR, 2>(s, lane & 4);
+    fold<DPP_XOR1, 1>(s, lane & 1);
+    s[0] += dpp_f64<DPP_XOR2>(s[0]);
 #pragma unroll
-    for (int half = UN / 2, bit = 1; half >= 1; half /= 2, bit *= 2) {
-      const bool odd = lane & bit;
-#pragma unroll
-      for (int i = 0; i < half; ++i) {
-        const double give = odd ? s[i] : s[i + half], keep = odd ? s[i + half] : s[i];
-        s[i] = keep + shfl_xor_f64(give, bit);
-      }
-    }
-#pragma unroll
-    for (int bit = UN; bit < LPB; bit *= 2) s[0] += shfl_xor_f64(s[0], bit);
-    // lane c < 8 of a block's has the sum of load: bits of c from the highest half down
-    const int i = (lane & 1) * 4 + (lane & 2) + ((lane >> 2) & 1), j = j0 + i * BPL + lane / LPB;
-    if (c < UN && j < cand) keys[j] = rank_of(s[0]);
+    for (int bit = 16; bit < LPB; bit *= 2) s[0] += shfl_xor_f64(s[0], bit);
+    const int at = j + ((c >> 1 & 4) + (c >> 1 & 2) + (c & 1)) * BPL + lane / LPB;
+    if (c < 16 && !(c & 2) && at < j1) keys[at] = rank_of(s[0]);
   }
-  __syncthreads();
-  // The first and last blocks are in; of the others the `need` highest, by halving an interval of ranks:
-  // at least `need` are at or above lo, fewer at or above hi.
-  const int head = a.first < cand ? a.first : cand, tail = cand - a.last > head ? cand - a.last : head;
-  const int need = a.count - head - (cand - tail);
+  return true;
+}
+
+// The first and last blocks are in; of the others, head .. tail - 1, the `need` highest.  They are found by halving
+// an interval of ranks: at least `need` are at or above lo, fewer at or above hi, until exactly `need` are
+// at or above its middle or lo is the last of them, whose equals are taken by the lowest numbers.
+struct Limits {
+  int head, tail, need;
+};
+__device__ __forceinline__ Limits limits_of(const SelectArgs& a, int cand) {
+  Limits l;
+  l.head = a.first < cand ? a.first : cand;
+  l.tail = cand - a.last > l.head ? cand - a.last : l.head;
+  l.need = a.count - l.head - (cand - l.tail);
+  return l;
+}
+
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)), lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  return (uint64_t)hi << 32 | lo;
+}
+
+// Exclusive sums of N counts in LDS, in place, by the first wave.
+template <int N>
+__device__ __forceinline__ void sum_counts(int* x) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < N; i += 64) {
+    const int y = i + lane < N ? x[i + lane] : 0;
+    int s = y;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int o = __shfl_up(s, off);
+      s = lane >= off ? s + o : s;
+    }
+    if (i + lane < N) x[i + lane] = before + s - y;
+    before += __shfl(s, 63);
+  }
+}
+
+// By W waves, K ranks a lane in registers: x[k] of number (k W + wave) 64 + lane.
+template <int K, int W>
+__device__ __forceinline__ void pick(const Limits& l, int cand, uint64_t* x, int32_t* list) {
+  __shared__ int cells[2][W], counts[K * W];
+  __shared__ uint64_t ends[2][W];
+  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
   uint64_t lo = ~0ull, hi = 0;
-  for (int j = head + tid; j < tail; j += ST) {
-    const uint64_t x = keys[j];
-    lo = x < lo ? x : lo;
-    hi = x > hi ? x : hi;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = (k * W + wave) * 64 + lane;
+    const bool in = j >= l.head && j < l.tail;
+    lo = in && x[k] < lo ? x[k] : lo;
+    hi = in && x[k] > hi ? x[k] : hi;
+    if (!in) x[k] = 0;                       // (no limit that is counted against is 0)
   }
 #pragma unroll
   for (int off = 1; off < 64; off *= 2) {
-    const uint64_t x = __shfl_xor(lo, off), y = __shfl_xor(hi, off);
-    lo = x < lo ? x : lo;
-    hi = y > hi ? y : hi;
+    const uint64_t y = __shfl_xor(lo, off), z = __shfl_xor(hi, off);
+    lo = y < lo ? y : lo;
+    hi = z > hi ? z : hi;
   }
-  if (lane == 0) {
-    ends[0][wave] = lo;
-    ends[1][wave] = hi;
-  }
-  __syncthreads();
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      ends[0][wave] = lo;
+      ends[1][wave] = hi;
+    }
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < SW; ++w) {
-    lo = ends[0][w] < lo ? ends[0][w] : lo;
-    hi = ends[1][w] > hi ? ends[1][w] : hi;
+    for (int w = 0; w < W; ++w) {
+      lo = ends[0][w] < lo ? ends[0][w] : lo;
+      hi = ends[1][w] > hi ? ends[1][w] : hi;
+    }
   }
-  ++hi;
-  int ties = need, turn = 0;                    // of those equal to lo, the lowest numbers
-  if (need <= 0) {
+  lo = uniform(lo);
+  hi = uniform(hi) + 1;
+  int ties = l.need;
+  if (l.need <= 0) {
     lo = hi;
     ties = 0;
   }
-  while (hi - lo > 1) {
+  for (int step = 0; hi - lo > 1; ++step) {
     const uint64_t mid = lo + (hi - lo) / 2;
-    int x = 0;
-    for (int j0 = head; j0 < tail; j0 += ST) x += __popcll(__ballot(j0 + tid < tail && keys[j0 + tid] >= mid));
-    x = count_all(x, cells[turn]);
-    turn ^= 1;
-    if (x >= need) lo = mid;
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) n += __popcll(__ballot(x[k] >= mid));
+    if constexpr (W > 1) {                   // (two cells in turn: one barrier a step)
+      if (lane == 0) cells[step & 1][wave] = n;
+      __syncthreads();
+      n = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) n += cells[step & 1][w];
+      n = __builtin_amdgcn_readfirstlane(n);
+    }
+    if (n >= l.need) lo = mid;
     else {
       hi = mid;
-      ties = need - x;
+      ties = l.need - n;
     }
-    if (x == need) {                            // exactly these
+    if (n == l.need) {
       --lo;
       ties = 0;
       break;
     }
   }
-  // in ascending order: above lo, and of those at lo the first `ties`
-  int at = 0, tied = 0;
-  for (int j0 = 0; j0 < cand; j0 += ST) {
-    const int j = j0 + tid;
-    const bool in = j < cand, forced = in && (j < head || j >= tail);
-    const uint64_t x = in ? keys[j] : 0;
-    const bool above = in && !forced && x > lo, equal = in && !forced && x == lo;
-    const uint64_t eq = __ballot(equal), below = (1ull << lane) - 1;
-    __syncthreads();
-    if (lane == 0) cells[0][wave] = __popcll(eq);
-    __syncthreads();
-    int before = tied;
+  const uint64_t below = (1ull << lane) - 1;
+  auto is_in = [&](int k) DC_INLINE {
+    const int j = (k * W + wave) * 64 + lane;
+    return j >= l.head && j < l.tail;
+  };
+  int first[K];
+  auto tally = [&](auto flag) DC_INLINE {       // first[k]: flags before number k of this wave's
+    int at = 0;
 #pragma unroll
-    for (int w = 0; w < SW; ++w) {
-      if (w < wave) before += cells[0][w];
-      tied += cells[0][w];
+    for (int k = 0; k < K; ++k) {
+      const int n = __popcll(__ballot(flag(k)));
+      first[k] = at;
+      at += n;
+      if (W > 1 && lane == 0) counts[k * W + wave] = n;
     }
-    const bool take = forced || above || (equal && before + __popcll(eq & below) < ties);
-    const uint64_t m = __ballot(take);
-    if (lane == 0) cells[1][wave] = __popcll(m);
-    __syncthreads();
-    int to = at;
+    if constexpr (W > 1) {
+      __syncthreads();
+      if (wave == 0) sum_counts<K * W>(counts);
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < SW; ++w) {
-      if (w < wave) to += cells[1][w];
-      at += cells[1][w];
+      for (int k = 0; k < K; ++k) first[k] = counts[k * W + wave];
     }
-    if (take) list[to + __popcll(m & below)] = j;
+  };
+  tally([&](int k) DC_INLINE { return is_in(k) && x[k] == lo; });
+  uint64_t taken = 0;                           // bit k: number k of this lane's is taken
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = (k * W + wave) * 64 + lane;
+    const bool in = is_in(k), equal = in && x[k] == lo;
+    const int before = first[k] + __popcll(__ballot(equal) & below);
+    if ((j < cand && !in) || (in && x[k] > lo) || (equal && before < ties)) taken |= 1ull << k;
   }
+  if constexpr (W > 1) __syncthreads();         // all have read the counts
+  tally([&](int k) DC_INLINE { return (taken >> k) & 1; });
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool take = (taken >> k) & 1;
+    const uint64_t m = __ballot(take);
+    if (take) list[first[k] + __popcll(m & below)] = (k * W + wave) * 64 + lane;
+  }
+}
+
+constexpr int ONE_WAVE = 512;            // most candidates that one wave picks among
+constexpr int ONE_LAUNCH = 1024;         // most of the kernel that also scores
+
+template <int K, int W>
+__device__ __forceinline__ void pick_from(const SelectArgs& a, const Choice& w, const uint64_t* keys) {
+  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
+  uint64_t x[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = (k * W + wave) * 64 + lane;
+    x[k] = j < w.cand ? keys[j] : 0;
+  }
+  pick<K, W>(limits_of(a, w.cand), w.cand, x, w.list);
+}
+
+// Lists whose choice is all candidates, or that no token has.
+__device__ __forceinline__ void pick_whole(const SelectArgs& a, const Choice& w) {
+  for (int i = threadIdx.x; i < a.count; i += blockDim.x) w.list[i] = i < w.cand ? i : -1;
+}
+
+// One workgroup per list.
+template <int DT, int D>
+__global__ void __launch_bounds__(ST) select_kernel(SelectArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  Choice w = choice_of(a, blockIdx.x);
+  uint64_t* keys = reinterpret_cast<uint64_t*>(lds);
+  if (!score_blocks<DT, D>(a, w, 0, MAX_BLOCKS, reinterpret_cast<double*>(lds), keys)) {
+    pick_whole(a, w);
+    return;
+  }
+  __syncthreads();
+  if (w.cand > ONE_WAVE) pick_from<ONE_LAUNCH / ST, SW>(a, w, keys);
+  else if (threadIdx.x < 64) w.cand <= 256 ? pick_from<4, 1>(a, w, keys) : pick_from<8, 1>(a, w, keys);
+}
+
+// Few lists of many blocks: `chunk` blocks of a list a workgroup to the workspace, then a workgroup per list.
+template <int DT, int D>
+__global__ void __launch_bounds__(ST) score_kernel(SelectArgs a) {
+  __shared__ double part[QG * 2 * D];
+  const int lists = a.batch * a.hk * a.groups, index = blockIdx.x % lists;
+  Choice w = choice_of(a, index);
+  score_blocks<DT, D>(a, w, (int)(blockIdx.x / lists) * a.chunk, a.chunk, part, a.keys + (size_t)index * a.ld_keys);
+}
+
+template <int K, int W>
+__global__ void __launch_bounds__(64 * W) pick_kernel(SelectArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bound = a.len >> a.bshift;
+  const uint64_t* keys = a.keys + (size_t)blockIdx.x * a.ld_keys;
+  uint64_t x[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {             // (within the longest unit's: the unit's own length is still on its way)
+    const int j = (k * W + wave) * 64 + lane;
+    x[k] = keys[j < bound ? j : bound - 1];
+  }
+  Choice w = choice_of(a, blockIdx.x);
+  candidates_of(a, w);
+  if (w.cand <= a.count) pick_whole(a, w);
+  else pick<K, W>(limits_of(a, w.cand), w.cand, x, w.list);
+}
+
+template <int K, int W>
+void launch_pick(const SelectArgs& a, int lists, hipStream_t s) {
+  hipLaunchKernelGGL((pick_kernel<K, W>), dim3((unsigned)lists), dim3(64 * W), 0, s, a);
 }
 
 template <int DT, int D>
 int select_type(const SelectArgs& a, hipStream_t s) {
-  constexpr int GROUPS = ST / RowT<DT, D>::LPR;
-  const int64_t rows = (int64_t)(a.share < a.tok.max_tokens ? a.share : a.tok.max_tokens) << a.gshift;
-  const size_t sums = (size_t)(rows < GROUPS ? rows : GROUPS) * 2 * D * 8, keys = (size_t)(a.len >> a.bshift) * 8;
-  const size_t bytes = sums > keys ? sums : keys;
+  const int lists = a.batch * a.hk * a.groups, blocks = a.len >> a.bshift;
+  const size_t ranks = (size_t)blocks * 8;
+  if (a.keys) {
+    hipLaunchKernelGGL((score_kernel<DT, D>), dim3((unsigned)(lists * ((blocks + a.chunk - 1) / a.chunk))), dim3(ST), 0, s,
+                       a);
+    if (blocks <= 256) launch_pick<4, 1>(a, lists, s);
+    else if (blocks <= ONE_WAVE) launch_pick<8, 1>(a, lists, s);
+    else if (blocks <= 1024) launch_pick<4, SW>(a, lists, s);
+    else if (blocks <= 2048) launch_pick<8, SW>(a, lists, s);
+    else if (blocks <= 4096) launch_pick<16, SW>(a, lists, s);
+    else launch_pick<MAX_BLOCKS / ST, SW>(a, lists, s);
+    return (int)hipGetLastError();
+  }
+  const size_t sums = QG * 2 * D * sizeof(double), bytes = sums > ranks ? sums : ranks;
   allow_lds((const void*)select_kernel<DT, D>, bytes);
-  hipLaunchKernelGGL((select_kernel<DT, D>), dim3((unsigned)(a.batch * a.hk * a.groups)), dim3(ST), bytes, s, a);
+  hipLaunchKernelGGL((select_kernel<DT, D>), dim3((unsigned)lists), dim3(ST), bytes, s, a);
   return (int)hipGetLastError();
 }
 
@@ -370,9 +551,21 @@ int launch_bounds(const BoundsArgs& a, int dtype, int D, void* stream) {
   return D == 128 ? bounds_type<0, 128>(a, s) : bounds_type<0, 64>(a, s);
 }
 
-bool select_fits(const SelectArgs& a, size_t& key_bytes) {
+bool select_plan(SelectArgs& a, size_t& key_bytes) {
+  const int blocks = a.len >> a.bshift;
+  const int64_t lists = (int64_t)a.batch * a.hk * a.groups;
   key_bytes = 0;
-  return (a.len >> a.bshift) <= MAX_BLOCKS && (int64_t)a.batch * a.hk * a.groups < (1 << 23);
+  a.chunk = 0;
+  if (blocks > MAX_BLOCKS || lists >= (1 << 23)) return false;
+  if (blocks > a.count && ((lists < CUS && blocks > ONE_WAVE) || blocks > ONE_LAUNCH)) {
+    // chunks that make about two workgroups a CU, of a step of the workgroup at least
+    const int64_t per = (2 * CUS + lists - 1) / lists;
+    const int64_t chunk = ((blocks + per - 1) / per + 63) / 64 * 64;
+    a.chunk = (int)chunk;
+    a.ld_keys = (blocks + 1) / 2 * 2;
+    key_bytes = ((size_t)lists * a.ld_keys * 8 + 255) & ~(size_t)255;
+  }
+  return true;
 }
 
 int launch_select(const SelectArgs& a, int dtype, int D, void* stream) {

@@ -236,12 +236,12 @@ struct SelectArgs {
   const void* bounds;
   const int32_t* unit_len;
   int32_t* list;            // [batch][groups][hk][count]
-  uint64_t* keys;           // [lists][ld_keys] ranks of the blocks
+  uint64_t* keys;           // [lists][ld_keys] ranks of the blocks, or null: one launch does it all
   int64_t cap;
   TokenArgs tok;
   int batch, n_layers, layer, hq, hk, gshift, len, bshift;
   int share, groups, count, first, last;
-  int ld_keys;
+  int ld_keys, chunk;       // blocks of a workgroup that scores
 };
 
 // The rows behind each unit's length become part of the cache (dc_rows.hip).
@@ -329,8 +329,8 @@ int launch_shared(const SharedArgs& a, int dtype, int D, void* stream);
 bool block_plan(BlockArgs& a, int dtype, int D, int L);
 int launch_blocks(const BlockArgs& a, int dtype, int D, void* stream);
 int launch_bounds(const BoundsArgs& a, int dtype, int D, void* stream);
-// Whether the launcher takes such a choice, and bytes of `keys`.
-bool select_fits(const SelectArgs& a, size_t& key_bytes);
+// How a choice is cut, and bytes of `keys`; false where the launcher does not take it.
+bool select_plan(SelectArgs& a, size_t& key_bytes);
 int launch_select(const SelectArgs& a, int dtype, int D, void* stream);
 
 }  // namespace dc
