@@ -8,7 +8,8 @@
 //   shared   sequences that have rows in common.  A softmax over two sets of keys is joined from the
 //            sets' maxima, sums and outputs, so the tokens of all sequences that share rows are the rows
 //            of the same tiles there, and those rows are read once for all of them; each
-//            sequence's own rows are a key range like a prompt's.  One launch holds both.
+//            sequence's own rows are a key range like a prompt's.  One launch holds both.  Where the
+//            sequences' own tokens fill tiles, a tile walks through both instead and nothing is joined.
 //   blocks   some blocks of the rows below len_u, from a list, then the rows behind the last complete
 //            block: a key's number goes through the list to its row where a tile is loaded, and is
 //            what the masks know.
@@ -243,7 +244,10 @@ struct Place {
   int start, total;             // rows before the tokens' own, and with them
   int rows, row0;               // (token, head) rows, the tile's first
   int split, k0, k1;            // the part of the keys: k0 .. k1 - 1
-  bool all;                     // (shared) a tile over the rows in common: every token sees them
+  // (shared) Keys are numbered through: the rows in common, `common` of them, 0 .. common - 1, then from `pad` on,
+  // a multiple of the key tile, the sequence's own.  A tile of rows of several sequences walks the former
+  // alone (pad beyond them), one of a sequence that has none the latter (pad 0).
+  int pu, common, pad;          // the prefix's unit
   int picked, behind;           // (blocks) rows of the chosen blocks, and the first row behind the complete blocks
 };
 
@@ -268,26 +272,51 @@ __device__ __forceinline__ void members_of(const SharedArgs& a, int p, int& f0, 
   n = n < 0 ? 0 : n < a.group_tokens ? n : a.group_tokens;
 }
 
-// Shared rows: one launch index per (row tile, key part, prefix and KV head), pairs fastest.
-__device__ __forceinline__ bool locate_shared(const SharedArgs& a, int bm, Place& w) {
+// The prefix of sequence b, or -1: the last one that begins at or before it, if it holds it.
+__device__ __forceinline__ int prefix_of(const SharedArgs& a, int b) {
+  int p = b / a.max_members;
+  if (a.first) {
+    const int lane = threadIdx.x & 63;
+    p = 0;
+    for (int p0 = 1; p0 < a.prefixes; p0 += 64) {
+      const int i = p0 + lane;
+      const uint64_t m = __ballot(i < a.prefixes && a.first[i < a.prefixes ? i : 0] <= b);
+      p += __popcll(m);
+      if (m != ~0ull) break;
+    }
+  }
+  if (p >= a.prefixes) return -1;
+  int f0, f1, t0, n;
+  members_of(a, p, f0, f1, t0, n);
+  return b >= f0 && b < f1 ? p : -1;
+}
+
+// Rows in common for the tokens of all sequences of a prefix: one launch index per (row tile, key part, prefix and
+// KV head), pairs fastest.  First what the keys are, then whose the rows.
+__device__ __forceinline__ bool locate_common(const SharedArgs& a, Place& w, int& tile, int& p) {
   const int pairs = a.prefixes * a.hk;
   const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int tile = rest / a.psplits, p = pair / a.hk;
-  int f0, f1;
-  w.all = true;
+  tile = rest / a.psplits;
+  p = pair / a.hk;
   w.split = rest % a.psplits;
   w.g = pair % a.hk;
-  w.u = (p * a.n_layers + a.layer) * a.hk + w.g;
+  w.u = 0;
+  w.pu = (p * a.n_layers + a.layer) * a.hk + w.g;
+  w.common = __builtin_amdgcn_readfirstlane(rows_before(a.punit_len, a.plen, w.pu));
+  w.pad = 1 << 30;
+  w.start = w.total = 0;
+  w.k0 = w.split * a.pchunk;
+  w.k1 = w.k0 + a.pchunk < w.common ? w.k0 + a.pchunk : w.common;
+  return w.k0 < w.k1;
+}
+__device__ __forceinline__ bool locate_members(const SharedArgs& a, int bm, int tile, int p, Place& w) {
+  int f0, f1;
   members_of(a, p, f0, f1, w.t0, w.n);
   w.t0 = __builtin_amdgcn_readfirstlane(w.t0);
   w.n = __builtin_amdgcn_readfirstlane(w.n);
   w.rows = w.n << a.gshift;
   w.row0 = tile * bm;
-  if (w.row0 >= w.rows) return false;
-  w.start = w.total = __builtin_amdgcn_readfirstlane(rows_before(a.punit_len, a.plen, w.u));
-  w.k0 = w.split * a.pchunk;
-  w.k1 = w.k0 + a.pchunk < w.total ? w.k0 + a.pchunk : w.total;
-  return w.k0 < w.k1;
+  return w.row0 < w.rows;
 }
 
 // The chosen blocks of one list in LDS: those entries, in order, that name one of the `cand` complete blocks
@@ -354,13 +383,11 @@ __device__ __forceinline__ bool locate_blocks(const BlockArgs& a, int bm, int* c
 // One launch index per (row tile, key part, sequence and KV head), the pairs fastest: with a
 // multiple of 8 of them a pair's workgroups share one XCD's L2.  The tiles with the most keys
 // go first.  False where nothing is to be done (the whole workgroup).
-template <int MODE>
+template <int MODE, int BN>
 __device__ __forceinline__ bool locate(const ArgsOf<MODE>& a, int bm, Place& w) {
   unsigned index = blockIdx.x;
   int splits = a.splits;
-  w.all = false;
   if constexpr (is_shared(MODE)) {
-    if (index < (unsigned)a.shared_wgs) return locate_shared(a, bm, w);
     index -= a.shared_wgs;
     splits -= a.psplits;
   }
@@ -380,10 +407,22 @@ __device__ __forceinline__ bool locate(const ArgsOf<MODE>& a, int bm, Place& w) 
   w.start = __builtin_amdgcn_readfirstlane(rows_before(a.unit_len, a.len, w.u));
   w.total = w.start + w.n;
   const int last = (w.row0 + bm < w.rows ? w.row0 + bm : w.rows) - 1;
-  const int kend = is_tree(MODE) ? w.total : w.start + (last >> a.gshift) + 1;   // keys any row of the tile sees
+  int kend = is_tree(MODE) ? w.total : w.start + (last >> a.gshift) + 1;   // keys any row of the tile sees
+  if constexpr (is_shared(MODE)) {
+    w.pu = w.common = w.pad = 0;
+    if (a.through) {
+      const int p = prefix_of(a, b);
+      if (p >= 0) {
+        w.pu = (p * a.n_layers + a.layer) * a.hk + w.g;
+        w.common = __builtin_amdgcn_readfirstlane(rows_before(a.punit_len, a.plen, w.pu));
+      }
+      w.pad = (w.common + BN - 1) / BN * BN;
+      kend += w.pad;
+    }
+  }
   w.k0 = w.split * a.chunk;
   w.k1 = w.k0 + a.chunk < kend ? w.k0 + a.chunk : kend;
-  if constexpr (is_shared(MODE)) w.split += a.psplits;     // behind the shared rows' parts
+  if constexpr (is_shared(MODE)) w.split += a.psplits;     // behind the parts of the rows in common
   return w.k0 < w.k1;
 }
 
@@ -427,9 +466,12 @@ __device__ __forceinline__ void ancestors(const AttendArgs& a, const Place& w, u
 // Which keys of the block kb .. kb + 31 token r sees.
 template <int MODE>
 __device__ __forceinline__ uint32_t sees32(const Place& w, const uint32_t* anc, int r, int kb) {
-  if (is_shared(MODE) && w.all) {
-    const int nv = w.total - kb;
-    return nv >= 32 ? ~0u : nv <= 0 ? 0u : (1u << nv) - 1u;
+  if constexpr (is_shared(MODE)) {
+    if (kb < w.pad) {
+      const int nv = w.common - kb;
+      return nv >= 32 ? ~0u : nv <= 0 ? 0u : (1u << nv) - 1u;
+    }
+    kb -= w.pad;
   }
   if constexpr (is_tree(MODE)) {
     const int d = kb - w.start;
@@ -572,20 +614,25 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
              w.split] = make_float2(NEG_INF, NO_PART);
       return;
     }
-  } else {
-    if (!locate<MODE>(a, C::BM, w)) return;
+  }
+  bool ahead = false;           // (shared) the first tile's loads go out before the rows are known
+  int mtile = 0, mp = 0;
+  if constexpr (is_shared(MODE)) {
+    if (blockIdx.x < (unsigned)a.shared_wgs) {
+      if (!locate_common(a, w, mtile, mp)) return;
+      ahead = mtile == 0;
+      if (!ahead && !locate_members(a, C::BM, mtile, mp, w)) return;
+    } else {
+      if (!locate<MODE, C::BN>(a, C::BM, w)) return;
+    }
+  } else if constexpr (MODE != BLOCKS) {
+    if (!locate<MODE, C::BN>(a, C::BM, w)) return;
   }
   const int k0 = w.k0, k1 = w.k1, total = w.total;
   // tile loads: 1024 bytes an instruction, the waves in turn; rows past the last are read as the last
   constexpr int LPW = C::TILE / 1024 / C::NW, RPI = 1024 / T::RB;    // instructions of a wave, rows of one
-  const char* kc = (const char*)a.k + ((size_t)w.u * a.cap + (MODE == BLOCKS ? 0 : k0)) * T::RB;
-  const char* vc = (const char*)a.v + ((size_t)w.u * a.cap + (MODE == BLOCKS ? 0 : k0)) * T::RB;
-  if constexpr (is_shared(MODE)) {
-    if (w.all) {
-      kc = (const char*)a.pk + ((size_t)w.u * a.pcap + k0) * T::RB;
-      vc = (const char*)a.pv + ((size_t)w.u * a.pcap + k0) * T::RB;
-    }
-  }
+  const char* kc = (const char*)a.k + ((size_t)w.u * a.cap + (MODE > TREE ? 0 : k0)) * T::RB;
+  const char* vc = (const char*)a.v + ((size_t)w.u * a.cap + (MODE > TREE ? 0 : k0)) * T::RB;
   const uint32_t lds0 = lds_offset(lds);
   uint32_t ko[LPW], vo[LPW];
 #pragma unroll
@@ -619,6 +666,30 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
       }
       return;
     }
+    if constexpr (is_shared(MODE)) {
+      const int kt = k0 + it * C::BN;          // a tile is of the rows in common or of the sequence's own
+      const bool own = kt >= w.pad;
+      const size_t at = own ? (size_t)(kt - w.pad) * T::RB : ((size_t)w.pu * a.pcap + kt) * T::RB;
+      const char *kt1 = (own ? kc : (const char*)a.pk) + at, *vt1 = (own ? vc : (const char*)a.pv) + at;
+      const int left = own ? total - (kt - w.pad) : w.common - kt;
+#pragma unroll
+      for (int x = 0; x < LPW; ++x) {
+        uint32_t back = 0;
+        if (left < C::BN) {
+          const int row = (x * C::NW + wave) * RPI + lane / T::CH;
+          if (row >= left) back = (row - left + 1) * T::RB;
+        }
+        const uint32_t dst = lds0 + buf * C::BUF + (x * C::NW + wave) * 1024;
+        if (a.once) {
+          load_to_lds16_at_nt(kt1, ko[x] - back, dst);
+          load_to_lds16_at_nt(vt1, vo[x] - back, dst + C::TILE);
+        } else {
+          load_to_lds16_at(kt1, ko[x] - back, dst);
+          load_to_lds16_at(vt1, vo[x] - back, dst + C::TILE);
+        }
+      }
+      return;
+    }
     const size_t at = (size_t)it * C::TILE;
     const int left = total - k0 - it * C::BN;
 #pragma unroll
@@ -640,6 +711,12 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
   };
   const int ntile = (k1 - k0 + C::BN - 1) / C::BN;
   load_tile(0, 0);        // under way while the rest is set up
+  if constexpr (is_shared(MODE)) {
+    if (ahead && !locate_members(a, C::BM, mtile, mp, w)) {
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");       // no load into LDS outlives its workgroup
+      return;
+    }
+  }
 
   // this lane's row
   const int wrow = w.row0 + 32 * rw;
@@ -655,10 +732,11 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
   int full = is_tree(MODE) ? w.start : w.start + wfirst + 1;   // keys below are seen by all its rows
   int some = is_tree(MODE) ? w.total : w.start + wlast + 1;    // keys from here on by none
   if constexpr (is_shared(MODE)) {
-    if (w.all) full = some = w.total;
+    full += w.pad;
+    some += w.pad;
   }
   if constexpr (is_tree(MODE)) {
-    if (!w.all) ancestors<C::THREADS>(a, w, anc, up);
+    if (!is_shared(MODE) || w.pad != 1 << 30) ancestors<C::THREADS>(a, w, anc, up);
   }
   // the Q rows are here before the first step: a wait that the compiler would otherwise place
   // behind the next tile's loads, and so for them
@@ -682,11 +760,15 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
       const int kt = k0 + it * C::BN;
       const int kb = kt + kw * SK;
       if (!active || kb >= k1 || kb >= some) return;
+      if constexpr (is_shared(MODE)) {
+        if (kb < w.pad && kb >= w.common) return;
+      }
       const char* kl = lds + BUF * C::BUF + kw * SK * T::RB;
       const char* vl = kl + C::TILE;
       f32x16_t s[SK / 32];
       float mx = NEG_INF;
-      const bool masked = kb + SK > full;
+      bool masked = kb + SK > full;
+      if constexpr (is_shared(MODE)) masked = kb < w.pad ? kb + SK > w.common : masked;
 #pragma unroll
       for (int x = 0; x < SK / 32; ++x) s[x] = scores32<DT, D>(kl + 32 * x * T::RB, qf, lane);
       if (masked) {
@@ -847,12 +929,14 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
 }
 
 // The same of shared rows or chosen blocks, whose parts are not all there: lane x holds place x's maximum and sum.
-// The first places' outputs are under way while the lengths say which hold a part (loads of the others are
-// of memory that is the call's, and dropped).
-template <int DT, int D, int MODE>
+// The first N places' outputs are under way while the lengths say which hold a part (loads of the others are
+// of memory that is the call's, and dropped).  Relaxed atomic loads are plain ones that the compiler leaves in their
+// place: others it moves behind the branches that the lengths decide (25 places of 32 rows: 5.3 -> 4.0 us).
+template <int DT, int D, int MODE, int N>
 __global__ void __launch_bounds__(256) places_join_kernel(ArgsOf<MODE> a) {
-  constexpr int EPL = D / 64, N = 16;
+  constexpr int EPL = D / 64;
   typedef float vec_t __attribute__((ext_vector_type(EPL)));
+  typedef std::conditional_t<EPL == 2, uint64_t, uint32_t> word_t;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pairs = a.batch * a.hk;
   const int pair = blockIdx.x % pairs, row = (blockIdx.x / pairs) * 4 + wave;
@@ -862,14 +946,16 @@ __global__ void __launch_bounds__(256) places_join_kernel(ArgsOf<MODE> a) {
   if (row >= n << a.gshift) return;
   const int r = row >> a.gshift, head = (g << a.gshift) + (row & ((1 << a.gshift) - 1));
   const size_t qrow = (size_t)(t0 + r) * a.hq + head;
-  const vec_t* po = reinterpret_cast<const vec_t*>(a.part + qrow * a.splits * D) + lane;
+  const word_t* po = reinterpret_cast<const word_t*>(a.part + qrow * a.splits * D) + lane;
   const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.tok.tokens * a.hq * a.splits * D) +
                      qrow * a.splits;
   float2 mine = ml[lane < a.splits ? lane : 0];
   vec_t v[N];
   auto load = [&](int s) DC_INLINE {
 #pragma unroll
-    for (int y = 0; y < N; ++y) v[y] = po[(size_t)(s + y < a.splits ? s + y : 0) * (D / EPL)];
+    for (int y = 0; y < N; ++y)
+      v[y] = __builtin_bit_cast(vec_t, __hip_atomic_load(po + (size_t)(s + y < a.splits ? s + y : 0) * (D / EPL),
+                                                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT));
   };
   load(0);
   bool live = lane < a.splits;
@@ -878,23 +964,19 @@ __global__ void __launch_bounds__(256) places_join_kernel(ArgsOf<MODE> a) {
   } else {
     const int u = (b * a.n_layers + a.layer) * a.hk + g;
     const int keys = rows_before(a.unit_len, a.len, u) + (a.parent ? n : r + 1);
-    int p = b / a.max_members, common = 0;
-    if (a.first) {                        // the last prefix that begins at or before sequence b
-      p = 0;
-      for (int p0 = 1; p0 < a.prefixes; p0 += 64) {
-        const int i = p0 + lane;
-        const uint64_t m = __ballot(i < a.prefixes && a.first[i < a.prefixes ? i : 0] <= b);
-        p += __popcll(m);
-        if (m != ~0ull) break;
+    const int p = prefix_of(a, b);
+    int common = p < 0 ? 0 : rows_before(a.punit_len, a.plen, (p * a.n_layers + a.layer) * a.hk + g);
+    if (a.through) {
+      live = live && lane < ((common + a.bn - 1) / a.bn * a.bn + keys + a.chunk - 1) / a.chunk;
+    } else {
+      if (p >= 0) {
+        int f0, f1, s0, sn;
+        members_of(a, p, f0, f1, s0, sn);
+        if (t0 + r < s0 || t0 + r >= s0 + sn) common = 0;
       }
+      live = live && (lane < a.psplits ? lane < (common + a.pchunk - 1) / a.pchunk
+                                       : lane - a.psplits < (keys + a.chunk - 1) / a.chunk);
     }
-    if (p < a.prefixes) {
-      int f0, f1, s0, sn;
-      members_of(a, p, f0, f1, s0, sn);
-      if (b >= f0 && b < f1 && t0 + r >= s0 && t0 + r < s0 + sn)
-        common = (rows_before(a.punit_len, a.plen, (p * a.n_layers + a.layer) * a.hk + g) + a.pchunk - 1) / a.pchunk;
-    }
-    live = live && (lane < a.psplits ? lane < common : lane - a.psplits < (keys + a.chunk - 1) / a.chunk);
   }
   if (!live) mine = make_float2(NEG_INF, 0.0f);
   const uint64_t there = __ballot(live);
@@ -910,10 +992,11 @@ __global__ void __launch_bounds__(256) places_join_kernel(ArgsOf<MODE> a) {
     if (s > 0) load(s);
 #pragma unroll
     for (int y = 0; y < N; ++y) {
-      if (s + y >= 64 || !((there >> (s + y)) & 1)) continue;
+      // (a select, not a branch: that would hold each load back until its turn)
+      const bool on = (there >> (s + y)) & 1;
       const float fy = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s + y));
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(v[y][e], fy, o[e]);
+      for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(on ? v[y][e] : 0.0f, fy, o[e]);
     }
   }
   float out[EPL];
@@ -926,6 +1009,34 @@ constexpr int CUS = 256;
 constexpr int MIN_CHUNK = 128;       // keys of a part, at least; a multiple of every key tile
 constexpr int64_t BIG_CACHE = 256ll << 20;      // the memory-side cache
 constexpr int MAX_PARTS = 64;        // of a key range: a lane each in the joining kernel
+
+// What a cut costs, for shared rows and chosen blocks, in us: constants that order the cuts of 76 calls of 1 to
+// 4000 tokens and 20 to 60000 rows as they were measured, 15 rows of tiles and parts each (what they choose
+// is slower than the best cut by 2 % on average and 18 % at most).  A workgroup starts and ends in 8, most of it a
+// chain of loads, and walks a tile of keys in `step`; two on a CU do not slow each other down, as loads bound
+// them.  Parts cost a launch and their bytes, written and read in float32.
+struct Cut {
+  int bm, bn, per_cu;
+  double step;
+};
+inline Cut cut_of(int dtype, int D, int bm, int64_t rows) {
+  const double filled = (double)(rows < bm ? rows : bm) / bm;
+  Cut c;
+  c.bm = bm;
+  c.bn = bm == 128 ? (dtype == 1 ? 64 : 32) : dtype == 1 || D == 64 ? 128 : 64;
+  // (workgroups of a CU by their LDS and registers, as in attend_plan)
+  c.per_cu = dtype == 1 ? (bm == 128 || D == 64 ? 2 : 1) : bm == 128 && D == 64 ? 2 : 1;
+  if (dtype == 1) c.step = bm == 128 ? 0.6 + 0.25 * D / 128 : 0.6 + 0.9 * D / 128;
+  else c.step = (bm == 128 ? 4.0 : 5.5) * D / 128;
+  if (bm == 128) c.step *= 1.0 + 0.35 * filled;
+  return c;
+}
+// rounds: of the workgroups on the card; steps: of the longest one; mean: of all.
+inline double cut_us(const Cut& c, double rounds, int64_t steps, double mean, int64_t parts, double outputs, int D) {
+  const double one = 8.0 + steps * c.step, all = rounds * (8.0 + mean * c.step);
+  return (one > all ? one : all) + (parts > 1 ? 2.5 + outputs * parts * D * 8 / 4e6 : 0.0);
+}
+constexpr int PARTS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
 
 template <int DT, int D, int RW, int KW, int SK, int MODE>
 int launch_mode(const ArgsOf<MODE>& a, int64_t wgs, hipStream_t s) {
@@ -952,8 +1063,13 @@ template <int DT, int D, int MODE>
 int launch_join(const ArgsOf<MODE>& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.tok.max_tokens << a.gshift;
   const dim3 grid((unsigned)(a.batch * a.hk * ((rows + 3) / 4)));
-  if constexpr (MODE > TREE) hipLaunchKernelGGL((places_join_kernel<DT, D, MODE>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attend_join_kernel<DT, D>), grid, dim3(256), 0, s, a);
+  if constexpr (MODE > TREE) {
+    const auto k = a.splits <= 4 ? places_join_kernel<DT, D, MODE, 4>
+                 : a.splits <= 8 ? places_join_kernel<DT, D, MODE, 8> : places_join_kernel<DT, D, MODE, 16>;
+    hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((attend_join_kernel<DT, D>), grid, dim3(256), 0, s, a);
+  }
   return (int)hipGetLastError();
 }
 

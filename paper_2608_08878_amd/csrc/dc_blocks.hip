@@ -122,9 +122,11 @@ template <int DT, int D>
 int bounds_type(const BoundsArgs& a, hipStream_t s) {
   const int n = (a.len >> a.bshift) - (a.from >> a.bshift);        // blocks of the longest unit
   if (n <= 0) return 0;
-  // a workgroup's waves take a few blocks each
-  int per = 4096 >> a.bshift;
-  per = per < 32 ? 32 : per;
+  // A workgroup's waves take a few blocks each: 4096 rows where there are many, a pass of each wave where there are few
+  // (700 rows of 6 float32 units 6.2 -> 4.6 us)
+  const int64_t share = (int64_t)n * a.units / (4 * CUS);
+  int per = share < 4096 >> a.bshift ? (int)share : 4096 >> a.bshift;
+  per = per < 8 ? 8 : (per + 7) / 8 * 8;
   const int gx = (n + per - 1) / per;
   for_grid_y(a.units, [&](int y0, int ny) {
     BoundsArgs b = a;
@@ -583,34 +585,34 @@ bool block_plan(BlockArgs& a, int dtype, int D, int L) {
   const int64_t keys = whole + (old < S - 1 ? old : S - 1) + a.tok.max_tokens;
   auto tiles = [&](int bm) { return lists * ((rows + bm - 1) / bm); };
   const int64_t bytes = lists * keys * 2 * D * (dtype == 1 ? 2 : 4);
-  // as in attend_plan
-  const bool stream = dtype == 1 && D == 128 && a.groups == 1 && bytes > BIG_CACHE / 4 * 3;
   const int64_t parts = (keys + MIN_CHUNK - 1) / MIN_CHUNK;
-  int bm = 128;
-  if (!stream && (rows <= 32 || tiles(128) * parts < CUS)) bm = 32;
-  else if (!stream && rows <= 64 && dtype == 1) bm = 64;
-  const int per_cu = dtype == 1 ? (bm == 128 || D == 64 ? 2 : 1) : bm == 128 && D == 64 ? 2 : 1;
   // (parts by the tiles of 128 at most, whatever the lengths: the workspace grows with the cache)
   int64_t most = 4 * CUS / tiles(128);
   most = most > parts ? parts : most;
   most = most > MAX_PARTS ? MAX_PARTS : most < 1 ? 1 : most;
-  const int bn = bm == 128 ? (dtype == 1 ? 64 : 32) : dtype == 1 || D == 64 ? 128 : 64;
-  const double step = dtype == 1 ? 0.5 + 0.8 * D / 128 : 3.6 * D / 128;
+  // Tiles and parts by their time; the lists are alike, so a last round of few workgroups is a whole one
   double least = -1.0;
-  for (int64_t n = 1; n <= most; ++n) {
-    const int64_t c = ((keys + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK, real = (keys + c - 1) / c;
-    const int64_t wgs = tiles(bm) * real, rounds = (wgs + per_cu * CUS - 1) / (per_cu * CUS);
-    const double walk = (double)rounds * ((c + bn - 1) / bn) * step * (per_cu == 2 && wgs > CUS ? 1.55 : 1.0);
-    const double join = real > 1 ? 3.0 + (double)a.tok.tokens * a.hq * real * D * 8 / 3.5e6 : 0.0;
-    if (least < 0.0 || walk + join < least) {
-      least = walk + join;
+  for (int bm = 32; bm <= 128; bm *= 2) {
+    if (bm == 64 && dtype != 1) continue;
+    const Cut cut = cut_of(dtype, D, bm, rows);
+    const int64_t slots = cut.per_cu * CUS;
+    int64_t last = 0;
+    for (const int n : PARTS) {
+      const int64_t c = ((keys + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK, real = (keys + c - 1) / c;
+      if (real > most || c == last) continue;
+      last = c;
+      const int64_t wgs = tiles(bm) * real;
+      const double us = cut_us(cut, (double)((wgs + slots - 1) / slots), ((c < keys ? c : keys) + cut.bn - 1) / cut.bn,
+                               (double)keys / cut.bn / real, real, (double)a.tok.tokens * a.hq, D);
+      if (least >= 0.0 && us >= least) continue;
+      least = us;
+      a.bm = bm;
       a.splits = (int)real;
       a.chunk = (int)c;
     }
   }
   a.most_splits = (int)most;
-  a.bm = bm;
-  a.group_tiles = (int)((rows + bm - 1) / bm);
+  a.group_tiles = (int)((rows + a.bm - 1) / a.bm);
   a.ntiles = a.groups * a.group_tiles;
   a.once = a.ntiles == 1 && bytes > BIG_CACHE;
   return tiles(32) * most < (1 << 24) &&

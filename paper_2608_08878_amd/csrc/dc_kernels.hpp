@@ -209,6 +209,8 @@ struct SharedArgs : AttendArgs {
   int group_tokens;         // bound of the tokens of one prefix's sequences
   int psplits, pchunk;      // parts of the shared rows, pchunk each
   int shared_wgs;           // workgroups of the shared rows, which come first
+  int through;              // 1: a sequence's tiles walk the shared rows and its own (psplits, shared_wgs = 0)
+  int bn;                   // keys of a tile
 };
 
 // The same over chosen blocks of the rows (dc_blocks.hip).
