@@ -15,6 +15,7 @@ DC_F32, DC_BF16 = 0, 1
 STATUS = {0: "DC_OK", 1: "DC_ERR_NULL", 2: "DC_ERR_SHAPE", 3: "DC_ERR_UNSUPPORTED",
           4: "DC_ERR_CAPACITY", 5: "DC_ERR_BUDGET", 6: "DC_ERR_WORKSPACE", 7: "DC_ERR_HIP",
           8: "DC_ERR_VALUE", 9: "DC_ERR_SCRATCH"}
+ERR_WORKSPACE = 6
 
 
 class dc_dims(ctypes.Structure):

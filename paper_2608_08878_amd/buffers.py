@@ -356,10 +356,23 @@ class DecodeBuffers:
         if parent is not None:
             self._ints(parent, (tokens.tokens,), "parent")
         shared.update()
-        self.reserve_shared_workspace(tokens, shared, self.kv.len + tokens.max_tokens, stream)
-        B.dc_shared_attention(self.dims, self.kv, layer, tokens, parent, shared, q, out, self.ws, self.ws_bytes,
-                              self._stream_here(stream))
+        here = self._stream_here(stream)
+        self._with_workspace(
+            lambda: B.dc_shared_attention(self.dims, self.kv, layer, tokens, parent, shared, q, out, self.ws,
+                                          self.ws_bytes, here),
+            lambda: self.reserve_shared_workspace(tokens, shared, self.kv.len + tokens.max_tokens, stream))
         return out
+
+    def _with_workspace(self, call, reserve):
+        """The call, which enqueues nothing if the workspace is too small; then it grows.  (Asking for the size
+        ahead of every call costs the host as much as the call's own plan.)"""
+        try:
+            call()
+        except B.DCError as e:
+            if e.status != B.ERR_WORKSPACE:
+                raise
+            reserve()
+            call()
 
     def _like_heads(self):
         d = self.dims
@@ -410,9 +423,11 @@ class DecodeBuffers:
         else:
             with torch.cuda.stream(stream):
                 out = torch.empty(shape, dtype=torch.int32, device=self.k.device)
-        self.reserve_block_workspace(tokens, blocks, count, self.kv.len + tokens.max_tokens, share, stream)
-        B.dc_block_select(self.dims, self.kv, layer, tokens, blocks, B.dc_pick(count, share, first, last), q, out, self.ws,
-                          self.ws_bytes, self._stream_here(stream))
+        here, pick = self._stream_here(stream), B.dc_pick(count, share, first, last)
+        self._with_workspace(
+            lambda: B.dc_block_select(self.dims, self.kv, layer, tokens, blocks, pick, q, out, self.ws, self.ws_bytes,
+                                      here),
+            lambda: self.reserve_block_workspace(tokens, blocks, count, self.kv.len + tokens.max_tokens, share, stream))
         return out
 
     def block_attention(self, tokens, blocks, chosen, q, share=1, layer=0, out=None, stream=None):
@@ -424,9 +439,11 @@ class DecodeBuffers:
             raise ValueError("share must be at least 1 and chosen [batch][groups][n_kv_heads][count]")
         count = chosen.shape[3]
         self._ints(chosen, self._lists(tokens, count, share), "chosen")
-        self.reserve_block_workspace(tokens, blocks, count, self.kv.len + tokens.max_tokens, share, stream)
-        B.dc_block_attention(self.dims, self.kv, layer, tokens, blocks, B.dc_pick(count, share, 0, 0), chosen, q, out,
-                             self.ws, self.ws_bytes, self._stream_here(stream))
+        here, pick = self._stream_here(stream), B.dc_pick(count, share, 0, 0)
+        self._with_workspace(
+            lambda: B.dc_block_attention(self.dims, self.kv, layer, tokens, blocks, pick, chosen, q, out, self.ws,
+                                         self.ws_bytes, here),
+            lambda: self.reserve_block_workspace(tokens, blocks, count, self.kv.len + tokens.max_tokens, share, stream))
         return out
 
     def sparse_attention(self, tokens, blocks, q, count, share=1, first=0, last=0, layer=0, out=None, stream=None):

@@ -1036,7 +1036,7 @@ inline double cut_us(const Cut& c, double rounds, int64_t steps, double mean, in
   const double one = 8.0 + steps * c.step, all = rounds * (8.0 + mean * c.step);
   return (one > all ? one : all) + (parts > 1 ? 2.5 + outputs * parts * D * 8 / 4e6 : 0.0);
 }
-constexpr int PARTS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+constexpr uint32_t PARTS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
 
 template <int DT, int D, int RW, int KW, int SK, int MODE>
 int launch_mode(const ArgsOf<MODE>& a, int64_t wgs, hipStream_t s) {

@@ -595,14 +595,16 @@ bool block_plan(BlockArgs& a, int dtype, int D, int L) {
   for (int bm = 32; bm <= 128; bm *= 2) {
     if (bm == 64 && dtype != 1) continue;
     const Cut cut = cut_of(dtype, D, bm, rows);
-    const int64_t slots = cut.per_cu * CUS;
-    int64_t last = 0;
-    for (const int n : PARTS) {
-      const int64_t c = ((keys + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK, real = (keys + c - 1) / c;
-      if (real > most || c == last) continue;
+    const int64_t slots = cut.per_cu * CUS, all = tiles(bm);
+    const uint32_t walk = keys;
+    uint32_t last = 0;
+    for (const uint32_t n : PARTS) {
+      if (n > most) break;
+      const uint32_t c = ((walk + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK, real = (walk + c - 1) / c;
+      if (c == last) continue;
       last = c;
-      const int64_t wgs = tiles(bm) * real;
-      const double us = cut_us(cut, (double)((wgs + slots - 1) / slots), ((c < keys ? c : keys) + cut.bn - 1) / cut.bn,
+      const int64_t wgs = all * real;
+      const double us = cut_us(cut, (double)((wgs + slots - 1) / slots), ((c < walk ? c : walk) + cut.bn - 1) / cut.bn,
                                (double)keys / cut.bn / real, real, (double)a.tok.tokens * a.hq, D);
       if (least >= 0.0 && us >= least) continue;
       least = us;

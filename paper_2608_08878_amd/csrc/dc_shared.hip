@@ -39,18 +39,20 @@ bool shared_plan(SharedArgs& a, int dtype, int D, int L, int Lp) {
     const int64_t ptiles = tiles(bm, ppairs, prows), otiles = tiles(bm, pairs, rows);
     for (int through = 0; through < 2; ++through) {
       const Cut cut = cut_of(dtype, D, bm, through || rows > prows ? rows : prows);
-      const int64_t padded = (Lp + cut.bn - 1) / cut.bn * cut.bn, own = through ? padded + L : L;
-      const int64_t walk = through ? own : longest, slots = cut.per_cu * CUS;
-      const double keys = (double)otiles * own + (through ? 0.0 : (double)ptiles * Lp);
-      int64_t last = 0;
-      for (const int n : PARTS) {
-        const int64_t c = ((walk + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK;
-        const int64_t ps = through ? 0 : (Lp + c - 1) / c, os = (own + c - 1) / c;
+      // (32 bits: this is host time of every call)
+      const uint32_t padded = (Lp + cut.bn - 1u) / cut.bn * cut.bn, own = through ? padded + L : L;
+      const uint32_t walk = through ? own : longest;
+      const double keys = ((double)otiles * own + (through ? 0.0 : (double)ptiles * Lp)) / cut.bn;
+      uint32_t last = 0;
+      for (const uint32_t n : PARTS) {
+        if (n > most) break;
+        const uint32_t c = ((walk + n - 1) / n + MIN_CHUNK - 1) / MIN_CHUNK * MIN_CHUNK;
+        const uint32_t ps = through ? 0 : (Lp + c - 1) / c, os = (own + c - 1) / c;
         if (ps + os > most || c == last) continue;
         last = c;
-        const int64_t wgs = ptiles * ps + otiles * os;
-        const double us = cut_us(cut, (double)wgs / slots, ((c < walk ? c : walk) + cut.bn - 1) / cut.bn,
-                                 keys / cut.bn / wgs, ps + os, (double)a.tok.tokens * a.hq, D);
+        const double wgs = (double)ptiles * ps + (double)otiles * os;
+        const double us = cut_us(cut, wgs / (cut.per_cu * CUS), ((c < walk ? c : walk) + cut.bn - 1) / cut.bn, keys / wgs,
+                                 ps + os, (double)a.tok.tokens * a.hq, D);
         if (least >= 0.0 && us >= least) continue;
         least = us;
         a.bm = bm;
