@@ -677,7 +677,8 @@ typedef struct {
  * on are computed from its keys, the others left as they are.  After dc_commit_rows (or a
  * decode step) `from` is the rows that every unit had before; after an eviction, which moves
  * rows, 0.
- * Errors: DC_ERR_NULL, DC_ERR_SHAPE (from outside 0..kv->len), DC_ERR_UNSUPPORTED (rows, alignment). */
+ * Errors: DC_ERR_NULL, DC_ERR_SHAPE (from outside 0..kv->len), DC_ERR_UNSUPPORTED (rows, alignment, bounds that
+ * overlap the keys). */
 dc_status dc_block_bounds(const dc_dims *dims, const dc_kv *kv, const dc_blocks *blocks, int32_t from,
                           void *hip_stream);
 
@@ -701,10 +702,11 @@ typedef struct {
  * hi and lo the block's bounds: scale * score is at least the sum of the queries' logits with any
  * row of the block.  Formed in binary64; NaN ranks below every number.
  *   q     [N][n_q_heads][head_dim], dtype, contiguous: normed and rotated as the keys are
- *   list  written: the chosen blocks ascending, -1 behind them (and for groups without tokens)
+ *   list  written: the chosen blocks ascending, -1 behind them (and for groups without tokens); overlaps
+ *         neither q nor the bounds
  * Workspace: dc_block_workspace_bytes(dims, tokens, blocks, pick, kv->len + max_tokens), as above.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_VALUE (first, last), DC_ERR_WORKSPACE, DC_ERR_UNSUPPORTED (rows, count,
- * alignment, more than 16384 blocks of a unit, grids). */
+ * alignment, overlaps, more than 16384 blocks of a unit, grids). */
 dc_status dc_block_select(const dc_dims *dims, const dc_kv *kv, int32_t layer, const dc_tokens *tokens,
                           const dc_blocks *blocks, const dc_pick *pick, const void *q, int32_t *list, void *ws,
                           size_t ws_bytes, void *hip_stream);
@@ -715,6 +717,7 @@ dc_status dc_block_select(const dc_dims *dims, const dc_kv *kv, int32_t layer, c
  *   list   as dc_block_select leaves it, or the caller's own (one layer's choice serves others): of its entries
  *          those count that name a complete block and are above all such entries before them, so
  *          that no block counts twice.  pick->count and share say its layout; blocks->bounds is not read.
+ *          Does not overlap out.
  * Workspace: as dc_block_select.
  * Errors: those of dc_prompt_attention; DC_ERR_NULL (blocks, pick, list), DC_ERR_UNSUPPORTED and DC_ERR_VALUE
  * as dc_block_select. */

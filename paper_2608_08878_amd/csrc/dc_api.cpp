@@ -940,6 +940,11 @@ dc_status attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_t
   return dc::launch_attend(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
 }
 
+bool bytes_meet(const void* a, int64_t n, const void* b, int64_t m) {
+  return (uintptr_t)a < (uintptr_t)b + (uintptr_t)m && (uintptr_t)b < (uintptr_t)a + (uintptr_t)n;
+}
+int64_t element_bytes(const dc_dims* d) { return d->dtype == DC_BF16 ? 2 : 4; }
+
 // What the attentions take beside their key ranges.
 dc_status check_attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens, const void* q,
                        const void* out) {
@@ -1004,6 +1009,10 @@ dc_status check_blocks(const dc_dims* dims, const dc_blocks* b, bool bounds) {
   return aligned16(b->bounds) ? DC_OK : DC_ERR_UNSUPPORTED;
 }
 
+int64_t bounds_bytes(const dc_dims* dims, const dc_blocks* b) {
+  return units_of(dims) * (dims->capacity / b->rows) * 2 * dims->head_dim * element_bytes(dims);
+}
+
 int block_shift(int rows) { return rows == 16 ? 4 : rows == 32 ? 5 : rows == 64 ? 6 : 7; }
 
 dc_status check_pick(const dc_pick* p) {
@@ -1015,6 +1024,10 @@ dc_status check_pick(const dc_pick* p) {
 }
 
 int groups_of(const dc_tokens* t, int share) { return (int)(((int64_t)t->max_tokens + share - 1) / share); }
+
+int64_t list_bytes(const dc_dims* dims, const dc_tokens* t, const dc_pick* p) {
+  return (int64_t)dims->batch * groups_of(t, p->share) * dims->n_kv_heads * p->count * 4;
+}
 
 bool plan_blocks(const dc_dims* dims, const dc_tokens* t, const dc_blocks* b, const dc_pick* p, int L, dc::BlockArgs& a,
                  size_t& need) {
@@ -1252,6 +1265,9 @@ dc_status dc_block_bounds(const dc_dims* dims, const dc_kv* kv, const dc_blocks*
   st = check_blocks(dims, blocks, true);
   if (st != DC_OK) return st;
   if (!aligned16(kv->k)) return DC_ERR_UNSUPPORTED;
+  if (bytes_meet(kv->k, units_of(dims) * dims->capacity * dims->head_dim * element_bytes(dims), blocks->bounds,
+                 bounds_bytes(dims, blocks)))
+    return DC_ERR_UNSUPPORTED;
   dc::BoundsArgs a;
   memset(&a, 0, sizeof(a));
   a.k = kv->k;
@@ -1291,6 +1307,10 @@ dc_status dc_block_select(const dc_dims* dims, const dc_kv* kv, int32_t layer, c
   st = check_pick(pick);
   if (st != DC_OK) return st;
   if (!aligned16(q) || ((uintptr_t)list & 3)) return DC_ERR_UNSUPPORTED;
+  const int64_t written = list_bytes(dims, tokens, pick);
+  if (bytes_meet(list, written, q, (int64_t)tokens->tokens * dims->n_q_heads * dims->head_dim * element_bytes(dims)) ||
+      bytes_meet(list, written, blocks->bounds, bounds_bytes(dims, blocks)))
+    return DC_ERR_UNSUPPORTED;
   dc::SelectArgs a;
   size_t need = 0;
   if (!plan_select(dims, tokens, blocks, pick, kv->len, a, need)) return DC_ERR_UNSUPPORTED;
@@ -1316,6 +1336,9 @@ dc_status dc_block_attention(const dc_dims* dims, const dc_kv* kv, int32_t layer
   st = check_pick(pick);
   if (st != DC_OK) return st;
   if ((uintptr_t)list & 3) return DC_ERR_UNSUPPORTED;
+  if (bytes_meet(list, list_bytes(dims, tokens, pick), out,
+                 (int64_t)tokens->tokens * dims->n_q_heads * dims->head_dim * element_bytes(dims)))
+    return DC_ERR_UNSUPPORTED;
   dc::BlockArgs a;
   size_t need = 0;
   if (!plan_blocks(dims, tokens, blocks, pick, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;

@@ -79,7 +79,7 @@ def test_shared_workspace_is_exact_and_does_not_shrink():
     assert B.dc_shared_workspace_bytes(_dims(batch=0), t, s, 10) == 0
 
 
-def _blocks(rows=64, bounds=FAKE):
+def _blocks(rows=64, bounds=FAR + FAR):
     return B.dc_blocks(rows, bounds)
 
 
@@ -93,7 +93,8 @@ def bounds(dims=None, kv=None, b=None, start=0, no_b=False):
     (dict(b=_blocks(48)), UNSUPPORTED), (dict(b=_blocks(256)), UNSUPPORTED), (dict(b=_blocks(0)), UNSUPPORTED),
     (dict(b=_blocks(bounds=ODD)), UNSUPPORTED), (dict(kv=_kv(k=ODD)), UNSUPPORTED), (dict(start=-1), SHAPE),
     (dict(start=241), SHAPE), (dict(kv=_kv(301)), SHAPE), (dict(kv=_kv(-1)), SHAPE), (dict(dims=_dims(batch=0)), SHAPE),
-    (dict(dims=_dims(dtype=3)), UNSUPPORTED)])
+    (dict(dims=_dims(dtype=3)), UNSUPPORTED), (dict(b=_blocks(bounds=FAKE)), UNSUPPORTED),
+    (dict(b=_blocks(bounds=FAKE - 1024)), UNSUPPORTED)])
 def test_bounds_refuses(kw, status):
     assert bounds(**kw) == status
 
@@ -131,6 +132,8 @@ COMMON = [(dict(q=None), NULL), (dict(lst=None), NULL), (dict(no_b=True), NULL),
 
 @pytest.mark.parametrize("kw,status", COMMON + [
     (dict(no_kv=True), NULL), (dict(b=_blocks(bounds=None)), NULL), (dict(b=_blocks(bounds=ODD)), UNSUPPORTED),
+    (dict(lst=FAKE + 60 * 2048 - 4), UNSUPPORTED), (dict(b=_blocks(bounds=FAR)), UNSUPPORTED),       # overlaps
+    (dict(dims=_dims(capacity=70000), kv=_kv(70000)), WORKSPACE),          # few lists of many blocks
     (dict(dims=_dims(capacity=16385 * 16), kv=_kv(16385 * 16), b=_blocks(16)), UNSUPPORTED)])
 def test_select_refuses(kw, status):
     assert select(**kw) == status
@@ -139,7 +142,7 @@ def test_select_refuses(kw, status):
 @pytest.mark.parametrize("kw,status", COMMON + [
     (dict(out=None), NULL), (dict(kv=_kv(k=None)), NULL), (dict(kv=_kv(v=None)), NULL), (dict(out=ODD), UNSUPPORTED),
     (dict(out=FAKE), UNSUPPORTED), (dict(out=FAKE + 512), UNSUPPORTED), (dict(kv=_kv(291)), CAPACITY),
-    (dict(kv=_kv(v=ODD)), UNSUPPORTED), (dict(wsb=0), WORKSPACE), (dict(ws=ODD, wsb=BIG), UNSUPPORTED)])
+    (dict(lst=FAR + 16), UNSUPPORTED), (dict(lst=FAR - 16), UNSUPPORTED), (dict(kv=_kv(v=ODD)), UNSUPPORTED), (dict(wsb=0), WORKSPACE), (dict(ws=ODD, wsb=BIG), UNSUPPORTED)])
 def test_attention_refuses(kw, status):
     assert attention(**kw) == status
 
