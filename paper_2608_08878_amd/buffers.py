@@ -351,7 +351,7 @@ class DecodeBuffers:
         out = self._check_queries(tokens, q, out, stream)
         if shared.like != self._like_heads() or shared.device != self._device:
             raise ValueError("the prefixes must have the cache's layers, heads, head_dim, dtype and device")
-        if shared.sequences > self.dims.batch:
+        if shared.sequences > self.dims.batch or (not shared.first and shared.sequences < self.dims.batch):
             raise ValueError(f"prefixes of {shared.sequences} sequences for a cache of {self.dims.batch}")
         if parent is not None:
             self._ints(parent, (tokens.tokens,), "parent")
@@ -452,7 +452,7 @@ class DecodeBuffers:
         return self.block_attention(tokens, blocks, chosen, q, share, layer, out, stream)
 
 
-def make_shared(prefix: DecodeBuffers, members=None) -> B.dc_shared:
+def make_shared(prefix: DecodeBuffers, members) -> B.dc_shared:
     """The caches of `prefix` (one sequence each) as rows that sequences of another DecodeBuffers have in common:
     the first members[0] sequences those of prefix 0, the next members[1] those of prefix 1 and so on,
     sequences behind them none.  An int: so many each, which are then all sequences."""

@@ -238,6 +238,16 @@ struct Cfg {
   static_assert(TILE % 1024 == 0 && SK % 32 == 0, "tile shape");
 };
 
+// Shared rows and chosen blocks, tiles of 32 rows: each of the four waves has 32 keys of a tile to itself, in one
+// buffer of its own, and waits for nobody's loads but its own.  K of the next tile is under way from when the scores are
+// formed, V from when the sums are, so that one of them always is.
+template <typename C, int MODE>
+constexpr bool ALONE = MODE > TREE && C::BM == 32;
+template <typename C, int MODE>
+constexpr int LDS_OF = ALONE<C, MODE> ? C::BUF : C::LDS;
+template <typename C, int MODE>
+constexpr int WAVES_OF = ALONE<C, MODE> ? (2 * C::BUF <= 144 * 1024 ? 2 : 1) : C::WAVES;
+
 // Where a workgroup's row tile and keys are.
 struct Place {
   int u, g, t0, n;              // unit, KV head, first packed token and tokens of the sequence
@@ -593,7 +603,7 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const Place& w, 
 // without the waits 163.  The rest of that call is the lengths: parts are cut by the longest cache, so the
 // shorter ones' last workgroups leave at once (16 caches of 16384 rows, 1.07 GB, one token each: 171).
 template <int DT, int D, int RW, int KW, int SK, int MODE>
-__global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES)) attend_kernel(ArgsOf<MODE> a) {
+__global__ void __launch_bounds__(64 * RW * KW, (WAVES_OF<Cfg<DT, D, RW, KW, SK>, MODE>)) attend_kernel(ArgsOf<MODE> a) {
   using T = KVT<DT, D>;
   using C = Cfg<DT, D, RW, KW, SK>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -709,8 +719,78 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
       }
     }
   };
+  // (alone) K or V of the wave's 32 keys of a tile, rows past the last as the last
+  constexpr bool OWN = ALONE<C, MODE>;
+  constexpr int LPO = OWN ? 32 * T::RB / 1024 : 1;
+  uint32_t oko[LPO], ovo[LPO];
+  const uint32_t own0 = lds0 + wave * 64 * T::RB;
+  if constexpr (OWN) {
+#pragma unroll
+    for (int x = 0; x < LPO; ++x) {
+      const int row = x * RPI + lane / T::CH, p = lane % T::CH;
+      oko[x] = row * T::RB + (p ^ T::kx(row)) * 16;
+      ovo[x] = row * T::RB + (p ^ T::vx(row)) * 16;
+    }
+  }
+  // the 32 keys in halves, each successive rows (a block has 16 rows at least): first row, and rows up to the last
+  const char* half_k[2];
+  const char* half_v[2];
+  int half_rows[2];
+  auto find_own = [&](int it) DC_INLINE {
+    const int kt = k0 + it * C::BN;
+    if constexpr (MODE == BLOCKS) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        int v = kt + kw * SK + 16 * j;
+        half_rows[j] = total - v < 1 ? 1 : total - v;
+        v = v < total ? v : total - 1;
+        const int block = __builtin_amdgcn_readfirstlane(chosen[1 + (v < w.picked ? v >> a.bshift : 0)]);
+        const int row = v < w.picked ? (block << a.bshift) + (v & ((1 << a.bshift) - 1)) : v - w.picked + w.behind;
+        half_k[j] = kc + (size_t)row * T::RB;
+        half_v[j] = vc + (size_t)row * T::RB;
+      }
+    } else if constexpr (is_shared(MODE)) {
+      const bool own = kt >= w.pad;
+      const int limit = own ? total : w.common;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        int row = (own ? kt - w.pad : kt) + kw * SK + 16 * j;
+        half_rows[j] = limit - row < 1 ? 1 : limit - row;
+        row = row < limit ? row : limit - 1;
+        const size_t at = (own ? (size_t)row : (size_t)w.pu * a.pcap + row) * T::RB;
+        half_k[j] = (own ? kc : (const char*)a.pk) + at;
+        half_v[j] = (own ? vc : (const char*)a.pv) + at;
+      }
+    }
+  };
+  auto load_own = [&](auto which) DC_INLINE {
+    constexpr bool V = decltype(which)::value;
+    const uint32_t dst = own0 + (V ? 32 * T::RB : 0);
+    uint32_t off[LPO];
+#pragma unroll
+    for (int x = 0; x < LPO; ++x) {
+      const int j = x * RPI / 16, rr = x * RPI % 16 + lane / T::CH;
+      off[x] = (V ? ovo[x] : oko[x]) - (16 * j + (rr >= half_rows[j] ? rr - half_rows[j] + 1 : 0)) * T::RB;
+    }
+    if (a.once) {
+#pragma unroll
+      for (int x = 0; x < LPO; ++x) load_to_lds16_at_nt((V ? half_v : half_k)[x * RPI / 16], off[x], dst + x * 1024);
+    } else {
+#pragma unroll
+      for (int x = 0; x < LPO; ++x) load_to_lds16_at((V ? half_v : half_k)[x * RPI / 16], off[x], dst + x * 1024);
+    }
+  };
+  auto load_first = [&]() DC_INLINE {
+    if constexpr (OWN) {
+      find_own(0);
+      load_own(std::false_type{});
+      load_own(std::true_type{});
+    } else {
+      load_tile(0, 0);
+    }
+  };
   const int ntile = (k1 - k0 + C::BN - 1) / C::BN;
-  load_tile(0, 0);        // under way while the rest is set up
+  load_first();           // under way while the rest is set up
   if constexpr (is_shared(MODE)) {
     if (ahead && !locate_members(a, C::BM, mtile, mp, w)) {
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");       // no load into LDS outlives its workgroup
@@ -803,7 +883,58 @@ __global__ void __launch_bounds__(64 * RW * KW, (Cfg<DT, D, RW, KW, SK>::WAVES))
           values32<DT, D>(vx, p, o, lane);
       }
     };
-    if constexpr (CAREFUL) load_tile(0, 0);
+    if constexpr (CAREFUL) load_first();
+    if constexpr (OWN) {
+      const char* kl = lds + wave * 64 * T::RB;
+      const char* vl = kl + 32 * T::RB;
+      for (int it = 0; it < ntile; ++it) {
+        const int kb = k0 + it * C::BN + kw * SK;
+        bool use = kb < k1 && kb < some, masked = kb + SK > full;
+        if constexpr (is_shared(MODE)) {
+          use = use && !(kb < w.pad && kb >= w.common);
+          masked = kb < w.pad ? kb + SK > w.common : masked;
+        }
+        // (loads are counted: all but the LPO of this tile's V are here)
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LPO) : "memory");
+        f32x16_t s;
+        Weights<DT> p;
+        if (use) s = scores32<DT, D>(kl, qf, lane);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        if (it + 1 < ntile) {
+          find_own(it + 1);
+          load_own(std::false_type{});
+        }
+        if (use) {
+          if (masked) mask32(s, sees32<MODE>(w, anc, r, kb), h);
+          float mx = NEG_INF;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
+          const float mn = fmaxf(m, half_max(mx) * c);
+          if (__any(mn > m + (CAREFUL ? 0.0f : SLACK))) {
+            const float f = rescale(m, mn);
+            l *= f;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[db][i] *= f;
+            m = mn;
+          }
+          const float mc = m == NEG_INF ? 0.0f : m;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -mc));
+          p.set(s, l);
+        }
+        if (it + 1 < ntile) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LPO) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        if (use) {
+          if (CAREFUL && masked) values32_masked<DT, D>(vl, s, sees32<MODE>(w, anc, r, kb), o, lane);
+          else values32<DT, D>(vl, p, o, lane);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        if (it + 1 < ntile) load_own(std::true_type{});
+      }
+      return;
+    }
     for (int it = 0; it < ntile; it += 2) {
       tile_step(it, std::integral_constant<int, 0>{});
       if (it + 1 < ntile) tile_step(it + 1, std::integral_constant<int, 1>{});
@@ -1010,30 +1141,29 @@ constexpr int MIN_CHUNK = 128;       // keys of a part, at least; a multiple of 
 constexpr int64_t BIG_CACHE = 256ll << 20;      // the memory-side cache
 constexpr int MAX_PARTS = 64;        // of a key range: a lane each in the joining kernel
 
-// What a cut costs, for shared rows and chosen blocks, in us: constants that order the cuts of 76 calls of 1 to
-// 4000 tokens and 20 to 60000 rows as they were measured, 15 rows of tiles and parts each (what they choose
-// is slower than the best cut by 2 % on average and 18 % at most).  A workgroup starts and ends in 8, most of it a
+// What a cut costs, for shared rows and chosen blocks, in us: constants that order the cuts of 92 calls of 1 to
+// 4000 tokens and 20 to 60000 rows, up to 90 of tile, parts and walk each, as they were measured (what they choose
+// is slower than the best cut by 1 % on average and 14 % at most).  A workgroup starts and ends in 7.5, most of it a
 // chain of loads, and walks a tile of keys in `step`; two on a CU do not slow each other down, as loads bound
 // them.  Parts cost a launch and their bytes, written and read in float32.
 struct Cut {
-  int bm, bn, per_cu;
+  int bn, per_cu;
   double step;
 };
 inline Cut cut_of(int dtype, int D, int bm, int64_t rows) {
-  const double filled = (double)(rows < bm ? rows : bm) / bm;
+  const double filled = (double)(rows < bm ? rows : bm) / bm, d = D / 128.0;
   Cut c;
-  c.bm = bm;
-  c.bn = bm == 128 ? (dtype == 1 ? 64 : 32) : dtype == 1 || D == 64 ? 128 : 64;
-  // (workgroups of a CU by their LDS and registers, as in attend_plan)
-  c.per_cu = dtype == 1 ? (bm == 128 || D == 64 ? 2 : 1) : bm == 128 && D == 64 ? 2 : 1;
-  if (dtype == 1) c.step = bm == 128 ? 0.6 + 0.25 * D / 128 : 0.6 + 0.9 * D / 128;
-  else c.step = (bm == 128 ? 4.0 : 5.5) * D / 128;
-  if (bm == 128) c.step *= 1.0 + 0.35 * filled;
+  c.bn = bm == 128 ? (dtype == 1 ? 64 : 32) : 128;
+  // (workgroups of a CU by their LDS and registers)
+  c.per_cu = dtype == 1 ? (bm == 64 && D == 128 ? 1 : 2) : D == 128 ? 1 : 2;
+  if (dtype == 1) c.step = bm == 128 ? 0.5 + 0.3 * d : (bm == 64 ? 1.6 : 1.2) * (0.4 + 0.6 * d);
+  else c.step = (bm == 128 ? 3.5 : 5.5) * d;
+  if (bm == 128) c.step *= 1.0 + 0.3 * filled;
   return c;
 }
 // rounds: of the workgroups on the card; steps: of the longest one; mean: of all.
 inline double cut_us(const Cut& c, double rounds, int64_t steps, double mean, int64_t parts, double outputs, int D) {
-  const double one = 8.0 + steps * c.step, all = rounds * (8.0 + mean * c.step);
+  const double one = 7.5 + steps * c.step, all = rounds * (7.5 + mean * c.step);
   return (one > all ? one : all) + (parts > 1 ? 2.5 + outputs * parts * D * 8 / 4e6 : 0.0);
 }
 constexpr uint32_t PARTS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
@@ -1042,20 +1172,22 @@ template <int DT, int D, int RW, int KW, int SK, int MODE>
 int launch_mode(const ArgsOf<MODE>& a, int64_t wgs, hipStream_t s) {
   using C = Cfg<DT, D, RW, KW, SK>;
   const auto k = attend_kernel<DT, D, RW, KW, SK, MODE>;
-  allow_lds((const void*)k, C::LDS);
-  hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(C::THREADS), C::LDS, s, a);
+  constexpr int lds = LDS_OF<C, MODE>;
+  allow_lds((const void*)k, lds);
+  hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(C::THREADS), lds, s, a);
   return (int)hipGetLastError();
 }
 
 // Row tiles of 32 rows with the keys cut among the waves, of 64 and two groups, or of 128 rows.
-// (float32 tiles of 32 rows of 128 elements: two key groups; what four need does not fit the LDS)
+// (float32 tiles of 32 rows of 128 elements: two key groups; what four need does not fit the LDS, but where waves
+// are alone)
 template <int DT, int D, int MODE>
 int launch_tiles(const ArgsOf<MODE>& a, int64_t wgs, hipStream_t s) {
   if constexpr (DT == 1)
     return a.bm == 32 ? launch_mode<DT, D, 1, 4, 32, MODE>(a, wgs, s)
          : a.bm == 64 ? launch_mode<DT, D, 2, 2, 64, MODE>(a, wgs, s) : launch_mode<DT, D, 4, 1, 64, MODE>(a, wgs, s);
   else
-    return a.bm == 32 ? launch_mode<DT, D, 1, D == 64 ? 4 : 2, 32, MODE>(a, wgs, s)
+    return a.bm == 32 ? launch_mode<DT, D, 1, (D == 64 || (MODE > TREE)) ? 4 : 2, 32, MODE>(a, wgs, s)
                       : launch_mode<DT, D, 4, 1, 32, MODE>(a, wgs, s);
 }
 
