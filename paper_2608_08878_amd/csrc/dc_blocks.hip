@@ -540,7 +540,7 @@ int select_type(const SelectArgs& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------ attention
-// 16 tokens over 64 of 512 blocks of 64 rows (32/8 heads of 128), 270 MB, 46.6 us = 5.8 TB/s and 4 for the join; 512
+// 16 tokens over 64 of 512 blocks of 64 rows (32/8 heads of 128), 270 MB, 46 us = 5.9 TB/s and 4.7 for the join; 512
 // tokens, 32 of them together over 64 blocks, 60 and 7: tile loads, most of them from beyond the L2.
 
 template <int DT, int D>
