@@ -618,3 +618,71 @@ def test_calls_are_repeatable_and_buffers_refuse():
         buf.block_attention(tok, blocks, torch.zeros((6, 1, 2, 3), device="cuda"), q)
     with pytest.raises(ValueError):
         buf.block_attention(tok, blocks, torch.zeros((6, 2, 2, 3), dtype=torch.int32, device="cuda"), q)
+
+
+def test_blocks_of_a_cache_that_decodes_and_evicts():
+    """Decode steps append rows and evictions move them: the bounds follow, and the blocks are those of the slots."""
+    from paper_2608_08878_amd.buffers import make_policy
+    g = torch.Generator().manual_seed(4)
+    buf = DecodeBuffers(2, 1, 8, 2, 128, 200)
+    buf.k.copy_(torch.randn(buf.k.shape, generator=g))
+    buf.v.copy_(torch.randn(buf.v.shape, generator=g))
+    buf.feat_init(150)
+    pol = make_policy((0.3 * torch.randn(4 * 32 + 32 + 32 + 1, generator=g)).cuda(), (32,))
+    blocks = buf.make_blocks(16)
+    buf.block_bounds(blocks)
+
+    def holds():
+        n, bd = buf.len // 16, np64(blocks.bounds_tensor)
+        return all(np.array_equal(bd[u, :n], ob.bounds(np64(buf.k[u, :buf.len]), 16, 3e38)) for u in range(4))
+
+    def heads(*shape):
+        return torch.randn(shape, generator=g).to(torch.bfloat16).cuda()
+
+    assert holds()
+    for _ in range(20):
+        before = buf.len
+        buf.decode_step(heads(4, 4, 128), heads(4, 128), heads(4, 128))
+        buf.block_bounds(blocks, before)
+        assert holds()
+    buf.decode_evict(pol, 90, heads(4, 4, 128), heads(4, 128), heads(4, 128))
+    assert buf.len == 90
+    buf.block_bounds(blocks)
+    assert holds()
+    tok, q = make_tokens([1, 1]), heads(2, 8, 128)
+    lists = buf.block_select(tok, blocks, q, 3)
+    out = buf.block_attention(tok, blocks, lists, q)
+    check_blocks(out, buf, [1, 1], [90] * 4, lists, q, 16, 1, "bf16")
+    buf.shrink(100)
+    with pytest.raises(ValueError):
+        buf.block_bounds(blocks)
+    again = buf.make_blocks(16)
+    buf.block_bounds(again)
+    assert torch.equal(again.bounds_tensor[:, :5], blocks.bounds_tensor[:, :5])
+
+
+def test_shared_rows_of_several_layers_and_shrunken_prefixes():
+    buf, pre, tok, sh, q, _, out, lens, plens = shared_case([1, 2, 1], [2, 1], 90, 20, layers=3, seed=21)
+    pre.shrink(92)
+    assert torch.equal(buf.shared_attention(tok, sh, q, layer=2), out)
+    for layer in range(3):
+        check_shared(buf.shared_attention(tok, sh, q, layer=layer), buf, pre, [1, 2, 1], [2, 1], lens, plens, q, "bf16",
+                     layer=layer)
+
+
+def test_workspaces_that_a_call_outgrows_stay_for_graphs():
+    buf, pre, tok, sh, q, _, out, _, _ = shared_case([1, 1], [2], 300, 20, seed=22)
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured = buf.shared_attention(tok, sh, q)
+    old = buf.ws_bytes
+    buf._grow(64 * old)                                  # as a later, larger call would
+    torch.full((old // 4,), float("nan"), device="cuda")
+    for _ in range(3):
+        captured.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(captured, want)
+        assert torch.equal(buf.shared_attention(tok, sh, q), want)
