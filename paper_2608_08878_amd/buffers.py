@@ -240,10 +240,10 @@ class DecodeBuffers:
 
     def _stream_here(self, stream):
         """The stream's handle; the cache has to be on the current device, which launches it."""
-        if torch.cuda.current_device() != self._device:
-            raise ValueError(f"the cache is on {self.k.device}, the current device is "
-                             f"cuda:{torch.cuda.current_device()}")
-        return stream_handle(stream)
+        here = torch.cuda.current_device()
+        if here != self._device:
+            raise ValueError(f"the cache is on {self.k.device}, the current device is cuda:{here}")
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(here)) if stream is None else stream_handle(stream)
 
     def _empty(self, shape, stream):
         """A tensor of the cache's type in memory that the given stream uses first (the allocator
