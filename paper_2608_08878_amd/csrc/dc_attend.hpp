@@ -723,6 +723,7 @@ __global__ void __launch_bounds__(64 * RW * KW, (WAVES_OF<Cfg<DT, D, RW, KW, SK>
   };
   // (alone) K or V of the wave's 32 keys of a tile, rows past the last as the last
   constexpr bool OWN = ALONE<C, MODE>;
+  static_assert(!OWN || (KW - 1) * C::OB <= LDS_OF<C, MODE>, "results fit the waves' buffers");
   constexpr int LPO = OWN ? 32 * T::RB / 1024 : 1;
   uint32_t oko[LPO], ovo[LPO];
   const uint32_t own0 = lds0 + wave * 64 * T::RB;

@@ -202,8 +202,9 @@ __device__ __forceinline__ void candidates_of(const SelectArgs& a, Choice& c) {
   if (c.cand) c.cand = __builtin_amdgcn_readfirstlane(rows_before(a.unit_len, a.len, c.u) >> a.bshift);
 }
 
-// Ranks of the blocks j0 .. j0 + chunk - 1 to keys[j], if there are such and a choice is to be made.  The scores are binary64: products of bf16 elements are exact there
-// and sums all but exact, so that a choice next to its limit does not hang on the order of a sum.
+// Ranks of the blocks j0 .. j0 + chunk - 1 to keys[j]; false if there are none or no choice is to be made.
+// The scores are binary64: products of bf16 elements are exact there and sums all but exact, so that a choice
+// next to its limit does not hang on the order of a sum.
 template <int DT, int D>
 __device__ __forceinline__ bool score_blocks(const SelectArgs& a, Choice& w, int j0, int chunk, double* part,
                                              uint64_t* keys) {
@@ -488,7 +489,8 @@ __global__ void __launch_bounds__(ST) select_kernel(SelectArgs a) {
   else if (threadIdx.x < 64) w.cand <= 256 ? pick_from<4, 1>(a, w, keys) : pick_from<8, 1>(a, w, keys);
 }
 
-// Few lists of many blocks (1562 for 8 lists: 4.7 + 7.7 us, in one launch 45): `chunk` blocks of a list a workgroup to the workspace, then a workgroup per list.
+// Few lists of many blocks (1562 for 8 lists: 4.7 + 7.7 us, in one launch 45): `chunk` blocks of a list a
+// workgroup to the workspace, then a workgroup per list.
 template <int DT, int D>
 __global__ void __launch_bounds__(ST) score_kernel(SelectArgs a) {
   __shared__ double part[QG * 2 * D];
@@ -586,7 +588,8 @@ bool block_plan(BlockArgs& a, int dtype, int D, int L) {
   const int64_t share = a.share < a.tok.max_tokens ? a.share : a.tok.max_tokens, rows = share << a.gshift;
   const int64_t lists = (int64_t)a.batch * a.hk * a.groups;
   // keys of a list: the chosen blocks, and the rows behind the complete ones
-  const int64_t old = L - a.tok.max_tokens, whole = (int64_t)a.count * S < old / S * S ? (int64_t)a.count * S : old / S * S;
+  const int64_t old = L - a.tok.max_tokens, chosen = (int64_t)a.count * S;
+  const int64_t whole = chosen < old / S * S ? chosen : old / S * S;
   const int64_t keys = whole + (old < S - 1 ? old : S - 1) + a.tok.max_tokens;
   auto tiles = [&](int bm) { return lists * ((rows + bm - 1) / bm); };
   const int64_t bytes = lists * keys * 2 * D * (dtype == 1 ? 2 : 4);
