@@ -123,11 +123,11 @@ template <int DT, int D>
 int bounds_type(const BoundsArgs& a, hipStream_t s) {
   const int n = (a.len >> a.bshift) - (a.from >> a.bshift);        // blocks of the longest unit
   if (n <= 0) return 0;
-  // A workgroup's waves take a few blocks each: 4096 rows where there are many, a pass of each wave where there are few
-  // (700 rows of 6 float32 units 6.2 -> 4.6 us)
-  const int64_t share = (int64_t)n * a.units / (4 * CUS);
-  int per = share < 4096 >> a.bshift ? (int)share : 4096 >> a.bshift;
-  per = per < 8 ? 8 : (per + 7) / 8 * 8;
+  // A workgroup's waves take one pass each, two where that still makes two workgroups a CU (4096 rows of 8 units of 128
+  // bf16: 3.8 and 5.1 us; of 32 units of 8192 rows 12.4 and 11.6, with 16 passes 33.6)
+  constexpr int RPI = 64 / RowT<DT, D>::LPR;
+  const int loads = (1 << a.bshift) / RPI, pass = BT / 64 * (loads < 8 ? 8 / loads : 1);
+  const int per = (int64_t)n * a.units >= 4 * CUS * pass ? 2 * pass : pass;
   const int gx = (n + per - 1) / per;
   for_grid_y(a.units, [&](int y0, int ny) {
     BoundsArgs b = a;
