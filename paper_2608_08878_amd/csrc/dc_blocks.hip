@@ -473,8 +473,9 @@ __device__ __forceinline__ void pick_whole(const SelectArgs& a, const Choice& w)
 }
 
 // One workgroup per list.  64 of up to 512 blocks for 128 lists 13 us (in two launches 8.9 + 5.9): latency of queries and
-// first bounds, then about 1 us for every 64 blocks.  1056 lists of 256 blocks 20 us, 7 of them vector
-// instructions in binary64 (its products run at the vector rate on the matrix cores too, so they stay here).
+// first bounds, then about 1 us for every 64 blocks, the vector instructions of the list's CU (512 and 1024 threads take
+// 12.8 and 12.9).  1056 lists of 256 blocks 20 us, with 512 threads 25.  (Matrix cores form binary64 products at
+// the vector rate, so they stay here.)
 template <int DT, int D>
 __global__ void __launch_bounds__(ST) select_kernel(SelectArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
