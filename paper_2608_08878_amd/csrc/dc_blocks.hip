@@ -52,7 +52,7 @@ constexpr uint32_t BOTTOM = DT == 1 ? 0x80808080u : 0x80800000u;
 
 constexpr int BT = 256;
 
-// One pass over the keys: 128 units of 16384 rows of 128 bf16, 554 MB, 92 us = 6.0 TB/s, of the 6.3 that reads reach.
+// One pass over the keys: 128 units of 16384 rows of 128 bf16, 554 MB, 90 us = 6.1 TB/s, of the 6.3 that reads reach.
 // A wave takes NB blocks at a time, 16 bytes a lane, LPR lanes a row.  Infinite elements and NaN count as the
 // largest numbers of their sign: scores of finite queries stay finite, and a block that holds
 // one ranks high rather than out of sight.

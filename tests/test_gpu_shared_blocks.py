@@ -327,6 +327,32 @@ def test_select_of_many_blocks(dtype, D, n, rows, count):
     assert np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("blocks", [5, 64, 255, 256, 257, 511, 512, 513, 1023, 1024, 1025, 2049, 4097])
+def test_select_at_the_sizes_where_the_search_changes(blocks):
+    n = 16 * blocks + 3
+    for batch, counts in ((1, (1, 4)), (40, (4,))):       # few lists, and more than half the CUs' number of heads
+        if batch * blocks > 42000:
+            continue
+        buf, bl, tok, q, lens = select_case([1] * batch, n, 16, 0, D=64, hk=8 if batch > 1 else 2, G=2, seed=blocks)
+        for count in counts + (blocks - 1, blocks):
+            if count > 2048 or batch > 1 and count > 4:
+                continue
+            for first, last in ((0, 0), (1, 3), (count, 0), (0, count), (min(2, count), 0)):   # (all of them forced, too)
+                if first + last > count:
+                    continue
+                got = buf.block_select(tok, bl, q, count, first=first, last=last)
+                want = chosen_by_oracle(buf, bl.bounds_tensor, [1] * batch, q, 16, lens, count, 1, first, last, 0)
+                assert np.array_equal(got.cpu().numpy(), want), (batch, count, first, last)
+        # seven kinds of blocks, so that the limit falls among equals; then all equal
+        x, count = bl.bounds_tensor, min(blocks, 2048) // 2 + 1
+        x.copy_(x[:, torch.arange(x.shape[1], device="cuda") % 7])
+        for _ in range(2):
+            got = buf.block_select(tok, bl, q, count, first=1)
+            want = chosen_by_oracle(buf, x, [1] * batch, q, 16, lens, count, 1, 1, 0, 0)
+            assert np.array_equal(got.cpu().numpy(), want), (batch, count)
+            q.zero_()
+
+
 def test_select_ties_and_values_that_are_no_numbers():
     buf, blocks, tok, q, lens = select_case([1, 1, 1], 600, 16, 9, hk=1, G=4, seed=3)
     # equal blocks: the lower numbers, by threes
