@@ -1286,11 +1286,14 @@ size_t dc_block_workspace_bytes(const dc_dims* dims, const dc_tokens* tokens, co
   if (check_tokens(dims, tokens) != DC_OK || check_blocks(dims, blocks, false) != DC_OK || check_pick(pick) != DC_OK ||
       max_len < tokens->max_tokens)
     return 0;
+  // Each call's own: one may be refused (grids, blocks of a unit) where the other is not, and a choice that is
+  // refused at max_len is not over shorter caches.
   dc::BlockArgs a;
   dc::SelectArgs c;
   size_t need = 0, keys = 0;
-  if (!plan_blocks(dims, tokens, blocks, pick, max_len, a, need)) return 0;
-  if (!plan_select(dims, tokens, blocks, pick, max_len - tokens->max_tokens, c, keys)) keys = 0;   // (refused)
+  if (!plan_blocks(dims, tokens, blocks, pick, max_len, a, need)) need = 0;
+  const int32_t rows = max_len - tokens->max_tokens, most = dc::select_max_blocks() * blocks->rows;
+  if (!plan_select(dims, tokens, blocks, pick, rows < most ? rows : most, c, keys)) keys = 0;
   return need > keys ? need : keys;
 }
 

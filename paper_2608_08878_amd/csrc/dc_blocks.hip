@@ -578,6 +578,8 @@ bool select_plan(SelectArgs& a, size_t& key_bytes) {
   return true;
 }
 
+int select_max_blocks() { return MAX_BLOCKS; }
+
 int launch_select(const SelectArgs& a, int dtype, int D, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (dtype == 1) return D == 128 ? select_type<1, 128>(a, s) : select_type<1, 64>(a, s);

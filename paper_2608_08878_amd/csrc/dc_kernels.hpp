@@ -333,6 +333,7 @@ int launch_blocks(const BlockArgs& a, int dtype, int D, void* stream);
 int launch_bounds(const BoundsArgs& a, int dtype, int D, void* stream);
 // How a choice is cut, and bytes of `keys`; false where the launcher does not take it.
 bool select_plan(SelectArgs& a, size_t& key_bytes);
+int select_max_blocks();
 int launch_select(const SelectArgs& a, int dtype, int D, void* stream);
 
 }  // namespace dc
