@@ -652,8 +652,9 @@ typedef struct {
  * read for all its sequences together.
  * Workspace: dc_shared_workspace_bytes(dims, tokens, shared, kv->len + max_tokens) bytes, as for
  * dc_prompt_attention the call's alone until it has run.
+ * out overlaps nothing that the call reads, the prefixes' cache among it.
  * Errors: those of dc_prompt_attention, dc_tree_attention; DC_ERR_NULL (shared, its cache), DC_ERR_SHAPE (its
- * sizes), DC_ERR_UNSUPPORTED (its alignment, more than 2^24 units). */
+ * sizes), DC_ERR_UNSUPPORTED (its alignment, overlaps, more than 2^24 units). */
 dc_status dc_shared_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer, const dc_tokens *tokens,
                               const int32_t *parent, const dc_shared *shared, const void *q, void *out,
                               void *ws, size_t ws_bytes, void *hip_stream);
@@ -717,7 +718,7 @@ dc_status dc_block_select(const dc_dims *dims, const dc_kv *kv, int32_t layer, c
  *   list   as dc_block_select leaves it, or the caller's own (one layer's choice serves others): of its entries
  *          those count that name a complete block and are above all such entries before them, so
  *          that no block counts twice.  pick->count and share say its layout; blocks->bounds is not read.
- *          Does not overlap out.
+ *   out    overlaps nothing that the call reads: q, the list, the cache
  * Workspace: as dc_block_select.
  * Errors: those of dc_prompt_attention; DC_ERR_NULL (blocks, pick, list), DC_ERR_UNSUPPORTED and DC_ERR_VALUE
  * as dc_block_select. */

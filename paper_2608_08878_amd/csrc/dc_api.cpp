@@ -945,6 +945,24 @@ bool bytes_meet(const void* a, int64_t n, const void* b, int64_t m) {
 }
 int64_t element_bytes(const dc_dims* d) { return d->dtype == DC_BF16 ? 2 : 4; }
 
+// Whether the outputs of an attention share bytes with what the call reads: workgroups store
+// while others still read.
+struct Outputs {
+  const void* at;
+  int64_t bytes;
+  bool meet(const void* p, int64_t n) const { return p && bytes_meet(at, bytes, p, n); }
+  bool meet(const dc_kv* kv, int64_t units, int64_t capacity, int64_t row) const {
+    return meet(kv->k, units * capacity * row) || meet(kv->v, units * capacity * row) || meet(kv->unit_len, units * 4);
+  }
+};
+Outputs outputs_of(const dc_dims* d, const dc_tokens* t, const void* out) {
+  return {out, (int64_t)t->tokens * d->n_q_heads * d->head_dim * element_bytes(d)};
+}
+bool meets_cache(const dc_dims* d, const dc_kv* kv, const dc_tokens* t, const void* out) {
+  const Outputs o = outputs_of(d, t, out);
+  return o.meet(kv, units_of(d), d->capacity, d->head_dim * element_bytes(d)) || o.meet(t->cu, (int64_t)(d->batch + 1) * 4);
+}
+
 // What the attentions take beside their key ranges.
 dc_status check_attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens, const void* q,
                        const void* out) {
@@ -956,7 +974,10 @@ dc_status check_attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, cons
   if (st != DC_OK) return st;
   if (!aligned16(q) || !aligned16(out)) return DC_ERR_UNSUPPORTED;
   const int64_t width = (int64_t)dims->n_q_heads * dims->head_dim;
-  return overlap(dims, q, tokens->tokens, width, width, out, tokens->tokens, width, width) ? DC_ERR_UNSUPPORTED : DC_OK;
+  return overlap(dims, q, tokens->tokens, width, width, out, tokens->tokens, width, width) ||
+                 meets_cache(dims, kv, tokens, out)
+             ? DC_ERR_UNSUPPORTED
+             : DC_OK;
 }
 
 template <typename Args>
@@ -1234,6 +1255,13 @@ dc_status dc_shared_attention(const dc_dims* dims, const dc_kv* kv, int32_t laye
   if (!shared->kv->k || !shared->kv->v) return DC_ERR_NULL;
   if (!aligned16(shared->kv->k) || !aligned16(shared->kv->v)) return DC_ERR_UNSUPPORTED;
   if (parent && tokens->max_tokens > DC_TREE_MAX_NODES) return DC_ERR_UNSUPPORTED;
+  const Outputs o = outputs_of(dims, tokens, out);
+  if (o.meet(parent, (int64_t)tokens->tokens * 4)) return DC_ERR_UNSUPPORTED;
+  if (shared->kv->len > 0 &&
+      (o.meet(shared->kv, (int64_t)shared->prefixes * dims->n_layers * dims->n_kv_heads, shared->capacity,
+              dims->head_dim * element_bytes(dims)) ||
+       o.meet(shared->first, ((int64_t)shared->prefixes + 1) * 4)))
+    return DC_ERR_UNSUPPORTED;
   if (shared->kv->len == 0) return attend(dims, kv, layer, tokens, parent, q, out, ws, ws_bytes, hip_stream);
   dc::SharedArgs a;
   size_t need = 0;
