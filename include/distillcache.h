@@ -559,8 +559,8 @@ dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
  * slots behind the rows hold the tokens' own K/V (dc_qk_norm_rope): token r of a sequence
  * sees the unit's rows and the tokens 0..r.
  *   q    [N][n_q_heads][head_dim], dtype, contiguous
- *   out  the same shape: o = sum_i a_i v_i, a = softmax_i(scale q.k_i); overlaps neither q nor
- *        the cache
+ *   out  the same shape: o = sum_i a_i v_i, a = softmax_i(scale q.k_i); overlaps nothing that the
+ *        call reads: q, the cache and its lengths, the offsets (and parents)
  * Scores, maxima and sums are float32.  With DC_BF16 the weights exp(s - m), m a running maximum,
  * meet the values in bf16 (2^-8 of each at most), and the sum that divides is of the rounded ones:
  * relative errors of about 0.0018 where the output's own rounding alone gives 0.0016.  The sum over
@@ -570,7 +570,7 @@ dc_status dc_qk_norm_rope(const dc_dims *dims, const dc_kv *kv, int32_t layer,
  * Workspace: dc_tokens_workspace_bytes(dims, tokens, kv->len + max_tokens) bytes, the call's alone
  * until it has run: calls on other streams, and graphs that may replay at the same time, take others.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_CAPACITY, DC_ERR_WORKSPACE,
- * DC_ERR_UNSUPPORTED (alignment, q and out overlap, grids past 2^24 workgroups: batch x KV heads x tiles of
+ * DC_ERR_UNSUPPORTED (alignment, overlaps of out, grids past 2^24 workgroups: batch x KV heads x tiles of
  * 32 to 128 (token, head) rows of the longest sequence). */
 dc_status dc_prompt_attention(const dc_dims *dims, const dc_kv *kv, int32_t layer,
                               const dc_tokens *tokens, const void *q, void *out, void *ws,

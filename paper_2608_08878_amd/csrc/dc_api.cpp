@@ -911,35 +911,6 @@ bool plan_attend(const dc_dims* dims, const dc_tokens* t, int L, dc::AttendArgs&
   return ok;
 }
 
-dc_status attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens,
-                 const int32_t* parent, const void* q, void* out, void* ws, size_t ws_bytes,
-                 void* hip_stream) {
-  dc_status st = check_tokens(dims, tokens);
-  if (st != DC_OK) return st;
-  if (!q || !out) return DC_ERR_NULL;
-  if (layer < 0 || layer >= dims->n_layers) return DC_ERR_SHAPE;
-  st = check_rows(dims, kv, tokens);
-  if (st != DC_OK) return st;
-  if (!aligned16(q) || !aligned16(out) || q == out) return DC_ERR_UNSUPPORTED;
-  dc::AttendArgs a;
-  size_t need = 0;
-  if (!plan_attend(dims, tokens, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
-  if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
-  if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
-  const int64_t width = (int64_t)a.hq * dims->head_dim;
-  if (overlap(dims, q, tokens->tokens, width, width, out, tokens->tokens, width, width)) return DC_ERR_UNSUPPORTED;
-  a.q = q;
-  a.out = out;
-  a.k = kv->k;
-  a.v = kv->v;
-  a.unit_len = kv->unit_len;
-  a.parent = parent;
-  a.part = need ? (float*)ws : nullptr;
-  a.layer = layer;
-  a.len = kv->len;
-  return dc::launch_attend(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
-}
-
 bool bytes_meet(const void* a, int64_t n, const void* b, int64_t m) {
   return (uintptr_t)a < (uintptr_t)b + (uintptr_t)m && (uintptr_t)b < (uintptr_t)a + (uintptr_t)n;
 }
@@ -961,6 +932,37 @@ Outputs outputs_of(const dc_dims* d, const dc_tokens* t, const void* out) {
 bool meets_cache(const dc_dims* d, const dc_kv* kv, const dc_tokens* t, const void* out) {
   const Outputs o = outputs_of(d, t, out);
   return o.meet(kv, units_of(d), d->capacity, d->head_dim * element_bytes(d)) || o.meet(t->cu, (int64_t)(d->batch + 1) * 4);
+}
+
+dc_status attend(const dc_dims* dims, const dc_kv* kv, int32_t layer, const dc_tokens* tokens,
+                 const int32_t* parent, const void* q, void* out, void* ws, size_t ws_bytes,
+                 void* hip_stream) {
+  dc_status st = check_tokens(dims, tokens);
+  if (st != DC_OK) return st;
+  if (!q || !out) return DC_ERR_NULL;
+  if (layer < 0 || layer >= dims->n_layers) return DC_ERR_SHAPE;
+  st = check_rows(dims, kv, tokens);
+  if (st != DC_OK) return st;
+  if (!aligned16(q) || !aligned16(out) || q == out) return DC_ERR_UNSUPPORTED;
+  dc::AttendArgs a;
+  size_t need = 0;
+  if (!plan_attend(dims, tokens, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
+  if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
+  if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  const int64_t width = (int64_t)a.hq * dims->head_dim;
+  if (overlap(dims, q, tokens->tokens, width, width, out, tokens->tokens, width, width) ||
+      meets_cache(dims, kv, tokens, out) || outputs_of(dims, tokens, out).meet(parent, (int64_t)tokens->tokens * 4))
+    return DC_ERR_UNSUPPORTED;
+  a.q = q;
+  a.out = out;
+  a.k = kv->k;
+  a.v = kv->v;
+  a.unit_len = kv->unit_len;
+  a.parent = parent;
+  a.part = need ? (float*)ws : nullptr;
+  a.layer = layer;
+  a.len = kv->len;
+  return dc::launch_attend(a, dims->dtype, dims->head_dim, hip_stream) == 0 ? DC_OK : DC_ERR_HIP;
 }
 
 // What the attentions take beside their key ranges.
