@@ -393,14 +393,23 @@ class DecodeBuffers:
             raise ValueError("the blocks are those of another cache")
         self._here(x, "blocks")
 
+    @staticmethod
+    def _int32(**numbers):
+        """The C structs would take the low 32 bits of larger ones."""
+        for name, x in numbers.items():
+            if not -2**31 <= x < 2**31:
+                raise ValueError(f"{name} = {x} does not fit 32 bits")
+
     def block_bounds(self, blocks, start=0, stream=None):
         """The bounds of all complete blocks that hold a row from `start` on, every layer's: `start` is the rows
         that every unit had at the last call, or 0 after an eviction."""
         self._blocks_of(blocks)
+        self._int32(start=start)
         B.dc_block_bounds(self.dims, self.kv, blocks, start, self._stream_here(stream))
 
     def reserve_block_workspace(self, tokens, blocks, count, max_len: int, share=1, stream=None):
         """As reserve_tokens_workspace, for block_select and block_attention."""
+        self._int32(count=count, share=share)
         self._grow(B.dc_block_workspace_bytes(self.dims, tokens, blocks, B.dc_pick(count, share, 0, 0), max_len), stream)
 
     def _lists(self, tokens, count, share):
@@ -415,6 +424,7 @@ class DecodeBuffers:
         self._like(q, tokens, self.dims.n_q_heads, "q")
         if count < 1 or share < 1:
             raise ValueError("count and share must be at least 1")
+        self._int32(count=count, share=share, first=first, last=last)
         shape = self._lists(tokens, count, share)
         if out is not None:
             self._ints(out, shape, "out")
@@ -437,6 +447,7 @@ class DecodeBuffers:
         self._blocks_of(blocks)
         if share < 1 or chosen.dim() != 4:
             raise ValueError("share must be at least 1 and chosen [batch][groups][n_kv_heads][count]")
+        self._int32(share=share)
         count = chosen.shape[3]
         self._ints(chosen, self._lists(tokens, count, share), "chosen")
         here, pick = self._stream_here(stream), B.dc_pick(count, share, 0, 0)
