@@ -1020,7 +1020,7 @@ bool plan_shared(const dc_dims* dims, const dc_tokens* t, const dc_shared* s, in
   const int64_t most = (int64_t)s->max_members * t->max_tokens;
   a.group_tokens = (int)(most < t->tokens ? most : t->tokens);
   if (!dc::shared_plan(a, dims->dtype, dims->head_dim, L, a.plen > 0 ? a.plen : 1)) return false;
-  need = parts_bytes(dims, t, a, 0);
+  need = parts_bytes(dims, t, a, 1);
   return true;
 }
 
@@ -1268,15 +1268,15 @@ dc_status dc_shared_attention(const dc_dims* dims, const dc_kv* kv, int32_t laye
   dc::SharedArgs a;
   size_t need = 0;
   if (!plan_shared(dims, tokens, shared, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;
-  if (!ws || ws_bytes < need) return DC_ERR_WORKSPACE;
-  if (!aligned16(ws)) return DC_ERR_UNSUPPORTED;
+  if (need && (!ws || ws_bytes < need)) return DC_ERR_WORKSPACE;
+  if (need && !aligned16(ws)) return DC_ERR_UNSUPPORTED;
   a.q = q;
   a.out = out;
   a.k = kv->k;
   a.v = kv->v;
   a.unit_len = kv->unit_len;
   a.parent = parent;
-  a.part = (float*)ws;
+  a.part = need ? (float*)ws : nullptr;
   a.layer = layer;
   a.len = kv->len;
   a.pk = shared->kv->k;

@@ -30,8 +30,16 @@ bool shared_plan(SharedArgs& a, int dtype, int D, int L, int Lp) {
     return packed < nt ? packed : nt;
   };
   const int64_t bytes = (ppairs * Lp + pairs * L) * 2 * D * (dtype == 1 ? 2 : 4);
-  // Parts of a row at most: what fills the card by the shared rows' tiles of 128, whatever the lengths
-  int64_t most = 2 + 4 * CUS / tiles(128, ppairs, prows);
+  // Parts of a row at most: what fills the card by the shared rows' tiles of 128, whatever the lengths.  One, and so
+  // no workspace, where the sequences' own tiles of 128 fill the card twice over and are all full, or eight times over and
+  // are full to 98 %: there are as many tiles over the shared rows by themselves, and parts are worth nothing.
+  // Where sequences without a prefix must be among them, they leave the tiles too uneven for that.  (8 prompts of 2048
+  // tokens behind 16384 rows, 32/8 heads of 128, 4295 us, would have to bring 545 MB for parts that nobody writes.
+  // Of uneven prompts whose tiles are full to 95 %, some are up to 16 % faster in two parts.)
+  const int64_t own128 = tiles(128, pairs, rows);
+  const bool whole = (all == own128 * 128 ? own128 >= 4 * CUS : own128 >= 16 * CUS && all * 50 >= own128 * 128 * 49) &&
+                     (int64_t)a.prefixes * a.max_members >= a.batch;
+  int64_t most = whole ? 1 : 2 + 4 * CUS / tiles(128, ppairs, prows);
   most = most > MAX_PARTS ? MAX_PARTS : most;
   // Tiles and parts by their time.  Either parts of equal length of the shared rows, for tiles of all their
   // sequences' tokens, and of the own rows; or tiles of one sequence through both, which read the shared
@@ -76,7 +84,7 @@ bool shared_plan(SharedArgs& a, int dtype, int D, int L, int Lp) {
   a.shared_wgs = (int)(ppairs * pt * a.psplits);
   // a launch counts its threads in 32 bits: 2^24 workgroups of 256
   return (ppairs * ((prows + 31) / 32) + pairs * ((rows + 31) / 32)) * most < (1 << 24) &&
-         pairs * ((rows + 3) / 4) < (1 << 24);
+         (most == 1 || pairs * ((rows + 3) / 4) < (1 << 24));
 }
 
 int launch_shared(const SharedArgs& a, int dtype, int D, void* stream) {
