@@ -1,0 +1,46 @@
+"""The cuts that the GPU tests of shared rows and chosen blocks rely on: each of their sizes reaches the tiles that it is
+there for (host code, no GPU)."""
+import pytest
+
+from . import plan_cases as C
+from . import plans as P
+
+pytestmark = pytest.mark.skipif(not P.can_ask(), reason="library not built or no C++ compiler")
+
+
+def _check(cases, line):
+    got = P.ask([line(*args) for args, _ in cases.values()])
+    for (name, (_, (bm, through, parts, once))), (ok, *g) in zip(cases.items(), got):
+        assert ok and (g[0], g[1], g[3] > 1, g[4]) == (bm, through, parts, once), (name, g)
+
+
+def test_shared_cases_reach_their_tiles():
+    _check({**C.SHARED, **{"once " + k: v for k, v in C.SHARED_ONCE.items()}}, P.shared_line)
+
+
+def test_block_cases_reach_their_tiles():
+    _check({**C.BLOCKS, **{"once " + k: v for k, v in C.BLOCKS_ONCE.items()}}, P.blocks_line)
+
+
+def test_every_shape_of_a_tile_is_there():
+    """(32 rows: the small cases of the GPU tests.)  In float32 there are no tiles of 64 rows, and in bf16 none for heads of
+    128 that these plans choose."""
+    shared = {(a[0], a[1], e[0], e[1], e[2]) for a, e in C.SHARED.values()}
+    for through, parts in ((0, True), (1, False), (1, True)):
+        want = {("bf16", 64, 64), ("bf16", 64, 128), ("bf16", 128, 128), ("f32", 64, 128), ("f32", 128, 128)}
+        assert {s[:3] for s in shared if s[3:] == (through, parts)} == want
+    blocks = {(a[0], a[1], e[0], e[2]) for a, e in C.BLOCKS.values()}
+    for parts in (False, True):
+        assert {s[:3] for s in blocks if s[3] == parts} == want
+    # several waves of rows in a tile
+    for a, e in [*C.SHARED.values()]:
+        assert max(a[4]) * a[3] > 32 or sum(a[4]) * a[3] > 32
+    for a, e in [*C.BLOCKS.values()]:
+        assert min(max(a[4]), a[8]) * a[3] > 32
+
+
+def test_prompts_that_fill_the_card_take_one_part_whatever_the_lengths():
+    lines = [P.shared_line("bf16", 128, 8, 4, [2048] * 8, [8], plen, rows) for plen in (1, 100, 16384, 1 << 20)
+             for rows in (0, 700, 20000)]
+    for ok, bm, through, psplits, splits, _ in P.ask(lines):
+        assert ok and through == 1 and psplits == 0 and splits == 1
