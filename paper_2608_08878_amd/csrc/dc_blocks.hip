@@ -629,7 +629,7 @@ bool block_plan(BlockArgs& a, int dtype, int D, int L) {
   a.ntiles = a.groups * a.group_tiles;
   a.once = a.ntiles == 1 && bytes > BIG_CACHE;
   return tiles(32) * most < (1 << 24) &&
-         (int64_t)a.batch * a.hk * ((((int64_t)a.tok.max_tokens << a.gshift) + 3) / 4) < (1 << 24);
+         (most == 1 || (int64_t)a.batch * a.hk * ((((int64_t)a.tok.max_tokens << a.gshift) + 3) / 4) < (1 << 24));
 }
 
 int launch_blocks(const BlockArgs& a, int dtype, int D, void* stream) {

@@ -38,9 +38,9 @@ def test_it_does_not_fall_where_a_choice_is_refused(batch, tokens):
 
 
 def test_it_is_the_choice_s_where_the_attention_is_refused():
-    # 4 million tokens: the attention's join is past 2^24 workgroups, the choice's 2^21 lists are not
+    # 8 million tokens: the attention's tiles are 2^24 workgroups, the choice's lists 2^22
     dims = B.dc_dims(4096, 1, 64, 8, 128, 21000, B.DC_BF16, 0, 0.0)
-    tok, blocks, pick = B.dc_tokens(4096 * 1024, 1024, None), B.dc_blocks(16, None), B.dc_pick(48, 16, 0, 0)
+    tok, blocks, pick = B.dc_tokens(4096 * 2048, 2048, None), B.dc_blocks(16, None), B.dc_pick(48, 16, 0, 0)
     have = B.dc_block_workspace_bytes(dims, tok, blocks, pick, 20000)
-    assert _select(dims, tok, pick, 20000 - 1024, have) == UNSUPPORTED
-    assert _select(dims, tok, pick, 20000 - 1024, 0) == WORKSPACE
+    assert _select(dims, tok, pick, 20000 - 2048, have) == UNSUPPORTED
+    assert _select(dims, tok, pick, 20000 - 2048, 0) == WORKSPACE

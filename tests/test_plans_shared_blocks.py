@@ -44,3 +44,12 @@ def test_prompts_that_fill_the_card_take_one_part_whatever_the_lengths():
              for rows in (0, 700, 20000)]
     for ok, bm, through, psplits, splits, _ in P.ask(lines):
         assert ok and through == 1 and psplits == 0 and splits == 1
+
+
+def test_grids_of_joins_that_are_not_launched_refuse_nothing():
+    # 4 million tokens are 2^23 tiles of 32 rows and 2^26 workgroups of a join: taken, in one part
+    (ok, _, _, _, splits, _), (past, *_) = P.ask([P.blocks_line("bf16", 128, 8, 8, [n] * 4096, 3000, 16, 48, 16)
+                                                 for n in (1024, 2048)])
+    assert ok and splits == 1 and not past
+    (ok, _, _, _, splits, _), = P.ask([P.shared_line("bf16", 128, 8, 8, [32768] * 64, [64], 1000, 0)])
+    assert ok and splits == 1
