@@ -676,9 +676,11 @@ typedef struct {
 } dc_blocks;
 
 /* Brings the bounds up to date, all layers: those of every complete block that holds a row from `from`
- * on are computed from its keys, the others left as they are.  After dc_commit_rows (or a
- * decode step) `from` is the rows that every unit had before; after an eviction, which moves
- * rows, 0.
+ * on are computed from its keys, the others left as they are.  One `from` serves all units: after dc_commit_rows (or a
+ * decode step) the rows that the unit with the fewest had before; after an eviction, which moves
+ * rows, 0.  kv->len is that number for caches of equal lengths.  Of a ragged cache it is the bound of the longest unit, and
+ * as `from` would leave the bounds of shorter units' new blocks as they were: the caller knows the shortest
+ * unit's rows from its own counts, or gives 0.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE (from outside 0..kv->len), DC_ERR_UNSUPPORTED (rows, alignment, bounds that
  * overlap the keys). */
 dc_status dc_block_bounds(const dc_dims *dims, const dc_kv *kv, const dc_blocks *blocks, int32_t from,

@@ -402,7 +402,8 @@ class DecodeBuffers:
 
     def block_bounds(self, blocks, start=0, stream=None):
         """The bounds of all complete blocks that hold a row from `start` on, every layer's: `start` is the rows
-        that every unit had at the last call, or 0 after an eviction."""
+        that the unit with the fewest had at the last call, or 0 after an eviction.  (`len` is those of caches of equal
+        lengths; of a ragged cache it is the longest unit's bound, and shorter units' new blocks would be left out.)"""
         self._blocks_of(blocks)
         self._int32(start=start)
         B.dc_block_bounds(self.dims, self.kv, blocks, start, self._stream_here(stream))
