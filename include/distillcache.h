@@ -717,7 +717,7 @@ dc_status dc_block_select(const dc_dims *dims, const dc_kv *kv, int32_t layer, c
 
 /* Causal attention as dc_prompt_attention's over part of the rows: a token sees the rows of the blocks
  * that its group's list names, the rows behind the unit's last complete block, and its
- * sequence's tokens up to itself.
+ * sequence's tokens up to itself.  Drafted trees have no such call: dc_tree_attention reads the whole cache.
  *   list   as dc_block_select leaves it, or the caller's own (one layer's choice serves others): of its entries
  *          those count that name a complete block and are above all such entries before them, so
  *          that no block counts twice.  pick->count and share say its layout; blocks->bounds is not read.

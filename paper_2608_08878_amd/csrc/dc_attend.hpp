@@ -240,9 +240,9 @@ struct Cfg {
 
 // Shared rows and chosen blocks, tiles of 32 rows: each of the four waves has 32 keys of a tile to itself, in one
 // buffer of its own, and waits for nobody's loads but its own.  K of the next tile is under way from when the scores are
-// formed, V from when the sums are, so that one of them always is.  Against two buffers of shared tiles: one token over
-// 48 blocks of 64 rows 10.3 -> 9 us, 16 tokens over 64 blocks each 46.6 -> 46, 24 float32 lists of 47 blocks (128
-// elements, whose two buffers left room for two waves) 51 -> 30 with the join.
+// formed, V from when the sums are, so that one of them always is.  Against two buffers of shared tiles (medians of the
+// kernel): one token over 48 blocks of 64 rows 11.9 -> 9.3 us, 16 tokens over 64 blocks each 47.2 -> 46, 24 float32 lists of
+// 47 blocks (128 elements, whose two buffers left room for two waves) 45 -> 26.5.
 template <typename C, int MODE>
 constexpr bool ALONE = MODE > TREE && C::BM == 32;
 template <typename C, int MODE>

@@ -543,8 +543,9 @@ int select_type(const SelectArgs& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------ attention
-// 16 tokens over 64 of 512 blocks of 64 rows (32/8 heads of 128), 270 MB, 46 us = 5.9 TB/s and 4.7 for the join; 512
-// tokens, 32 of them together over 64 blocks, 60 and 7: tile loads, most of them from beyond the L2.
+// 16 tokens over 64 of 512 blocks of 64 rows (32/8 heads of 128), 270 MB, 46 us = 5.9 TB/s and 4.6 for the join; 512
+// tokens, 32 of them together over 64 blocks, 61 and 7.6: waits for tiles in 48 % of the waves' cycles (56 % of their
+// lines come from beyond the L2), and parts of the longest list that there may be, which are longer than these lists need.
 
 template <int DT, int D>
 int blocks_type(const BlockArgs& a, hipStream_t s) {

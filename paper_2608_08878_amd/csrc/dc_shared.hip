@@ -1,10 +1,10 @@
 // Attention of sequences that have rows in common: how a call is cut, and its launches (the kernels
 // are in dc_attend.hpp).
 //
-// Eight rollouts of 8192 rows (32/8 heads of 128, 40 MB) 13.1 us and 5.6 for the join: a workgroup's start, the
-// chain of lengths and first loads, is most of it (the walk is two tiles of keys).  59 sequences over four
-// prefixes of up to 16384 rows, 370 MB, 66 us = 5.6 TB/s, bound by HBM.  Eight prompts of 512 tokens behind
-// 16384 shared rows 1066-1100 us = 1.03 PFLOP/s, bound as the prompts are.
+// Eight rollouts of 8192 rows (32/8 heads of 128, 40 MB) 12.8 us and 5.6 for the join: a workgroup's start, the
+// chain of lengths and first loads, is most of it (the walk is two tiles of keys).  50 sequences over four
+// prefixes of up to 16384 rows, 370 MB, 67 us = 5.5 TB/s, bound by HBM.  Eight prompts of 512 tokens behind
+// 16384 shared rows 1076 us = 1.04 PFLOP/s, bound as the prompts are.
 #include "dc_attend.hpp"
 
 namespace dc {

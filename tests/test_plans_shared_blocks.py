@@ -53,3 +53,11 @@ def test_grids_of_joins_that_are_not_launched_refuse_nothing():
     assert ok and splits == 1 and not past
     (ok, _, _, _, splits, _), = P.ask([P.shared_line("bf16", 128, 8, 8, [32768] * 64, [64], 1000, 0)])
     assert ok and splits == 1
+
+
+def test_large_calls_of_single_tokens_take_tiles_of_32_rows():
+    """Two calls of test_gpu_shared_blocks by many workgroups: 197 and 147 MB of rows, under the 256 MiB from which rows are
+    read past the caches, so they run the tiles of 32 rows that smaller ones do (C.SHARED_ONCE, C.BLOCKS_ONCE are larger)."""
+    got = P.ask([P.shared_line("bf16", 128, 8, 4, [1] * 12, [6, 6], 15000, 1500),
+                 P.blocks_line("bf16", 128, 4, 4, [1] * 32, 2600, 64, 34, 1)])
+    assert [(g[1], g[5]) for g in got] == [(32, 0), (32, 0)]
