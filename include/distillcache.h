@@ -682,7 +682,7 @@ typedef struct {
  * as `from` would leave the bounds of shorter units' new blocks as they were: the caller knows the shortest
  * unit's rows from its own counts, or gives 0.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE (from outside 0..kv->len), DC_ERR_UNSUPPORTED (rows, alignment, bounds that
- * overlap the keys). */
+ * overlap the keys or the lengths). */
 dc_status dc_block_bounds(const dc_dims *dims, const dc_kv *kv, const dc_blocks *blocks, int32_t from,
                           void *hip_stream);
 
@@ -707,7 +707,7 @@ typedef struct {
  * row of the block.  Formed in binary64; NaN ranks below every number.
  *   q     [N][n_q_heads][head_dim], dtype, contiguous: normed and rotated as the keys are
  *   list  written: the chosen blocks ascending, -1 behind them (and for groups without tokens); overlaps
- *         neither q nor the bounds
+ *         nothing that the call reads: q, the bounds, the lengths, the offsets
  * Workspace: dc_block_workspace_bytes(dims, tokens, blocks, pick, kv->len + max_tokens), as above.
  * Errors: DC_ERR_NULL, DC_ERR_SHAPE, DC_ERR_VALUE (first, last), DC_ERR_WORKSPACE, DC_ERR_UNSUPPORTED (rows, count,
  * alignment, overlaps, more than 16384 blocks of a unit, grids). */

@@ -916,7 +916,7 @@ bool bytes_meet(const void* a, int64_t n, const void* b, int64_t m) {
 }
 int64_t element_bytes(const dc_dims* d) { return d->dtype == DC_BF16 ? 2 : 4; }
 
-// Whether the outputs of an attention share bytes with what the call reads: workgroups store
+// Whether outputs share bytes with what their call reads: workgroups store
 // while others still read.
 struct Outputs {
   const void* at;
@@ -1295,8 +1295,9 @@ dc_status dc_block_bounds(const dc_dims* dims, const dc_kv* kv, const dc_blocks*
   st = check_blocks(dims, blocks, true);
   if (st != DC_OK) return st;
   if (!aligned16(kv->k)) return DC_ERR_UNSUPPORTED;
-  if (bytes_meet(kv->k, units_of(dims) * dims->capacity * dims->head_dim * element_bytes(dims), blocks->bounds,
-                 bounds_bytes(dims, blocks)))
+  const Outputs o = {blocks->bounds, bounds_bytes(dims, blocks)};
+  if (o.meet(kv->k, units_of(dims) * dims->capacity * dims->head_dim * element_bytes(dims)) ||
+      o.meet(kv->unit_len, units_of(dims) * 4))
     return DC_ERR_UNSUPPORTED;
   dc::BoundsArgs a;
   memset(&a, 0, sizeof(a));
@@ -1340,9 +1341,9 @@ dc_status dc_block_select(const dc_dims* dims, const dc_kv* kv, int32_t layer, c
   st = check_pick(pick);
   if (st != DC_OK) return st;
   if (!aligned16(q) || ((uintptr_t)list & 3)) return DC_ERR_UNSUPPORTED;
-  const int64_t written = list_bytes(dims, tokens, pick);
-  if (bytes_meet(list, written, q, (int64_t)tokens->tokens * dims->n_q_heads * dims->head_dim * element_bytes(dims)) ||
-      bytes_meet(list, written, blocks->bounds, bounds_bytes(dims, blocks)))
+  const Outputs o = {list, list_bytes(dims, tokens, pick)};
+  if (o.meet(q, outputs_of(dims, tokens, q).bytes) || o.meet(blocks->bounds, bounds_bytes(dims, blocks)) ||
+      o.meet(kv->unit_len, units_of(dims) * 4) || o.meet(tokens->cu, (int64_t)(dims->batch + 1) * 4))
     return DC_ERR_UNSUPPORTED;
   dc::SelectArgs a;
   size_t need = 0;
@@ -1369,9 +1370,7 @@ dc_status dc_block_attention(const dc_dims* dims, const dc_kv* kv, int32_t layer
   st = check_pick(pick);
   if (st != DC_OK) return st;
   if ((uintptr_t)list & 3) return DC_ERR_UNSUPPORTED;
-  if (bytes_meet(list, list_bytes(dims, tokens, pick), out,
-                 (int64_t)tokens->tokens * dims->n_q_heads * dims->head_dim * element_bytes(dims)))
-    return DC_ERR_UNSUPPORTED;
+  if (outputs_of(dims, tokens, out).meet(list, list_bytes(dims, tokens, pick))) return DC_ERR_UNSUPPORTED;
   dc::BlockArgs a;
   size_t need = 0;
   if (!plan_blocks(dims, tokens, blocks, pick, kv->len + tokens->max_tokens, a, need)) return DC_ERR_UNSUPPORTED;

@@ -1,11 +1,11 @@
-"""Attention outputs inside what the call reads are refused: the caches' rows, lengths, parents and offsets (no GPU)."""
+"""Outputs inside what their call reads are refused: the caches' rows, lengths, parents and offsets (no GPU)."""
 import os
 
 import pytest
 
 from paper_2608_08878_amd import binding as B
 
-from .test_abi_shared_blocks import _dims, _shared, _tok, attention, shared
+from .test_abi_shared_blocks import _blocks, _dims, _shared, _tok, attention, bounds, select, shared
 
 pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="library not built")
 
@@ -57,3 +57,26 @@ def test_absent_arrays_meet_nothing():
     kv = B.dc_kv(K, V, 240, None)
     assert shared(kv=kv, s=_shared(B.dc_kv(PK, PV, 400, None)), q=Q, out=16) == WORKSPACE
     assert attention(kv=kv, q=Q, lst=LIST, out=16) == WORKSPACE
+
+
+BOUNDS_BYTES, LIST_BYTES = 36 * 4 * 2 * 128 * 2, 6 * 10 * 2 * 4 * 4      # blocks of 64 of 300 rows; 4 of them for every token
+
+
+@pytest.mark.parametrize("at,size", [(K, CACHE), (LENS, 36 * 4)])
+def test_bounds_refuse_what_they_read(at, size):
+    for b in (at - BOUNDS_BYTES + 16, at, at + (size - 1) // 16 * 16):
+        assert bounds(kv=KV, b=_blocks(bounds=b)) == UNSUPPORTED, hex(b)
+
+
+def _select(lst, **kw):
+    # (a long cache, whose choice takes a workspace: no call goes on to a launch)
+    return select(dims=_dims(capacity=70000), kv=B.dc_kv(None, None, 70000, LENS), tok=_tok(cu=CU), b=_blocks(bounds=1 << 36),
+                  q=Q, lst=lst)
+
+
+@pytest.mark.parametrize("at,size", [(LENS, 36 * 4), (CU, 7 * 4), (Q, OUT)])
+def test_choices_refuse_what_they_read(at, size):
+    for lst in (at - LIST_BYTES + 4, at, at + size - 4):
+        assert _select(lst) == UNSUPPORTED, hex(lst)
+    for lst in (at - LIST_BYTES, at + size):
+        assert _select(lst) == WORKSPACE
