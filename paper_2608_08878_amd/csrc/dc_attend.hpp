@@ -1065,7 +1065,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
 // The same of shared rows or chosen blocks, whose parts are not all there: lane x holds place x's maximum and sum.
 // The first N places' outputs are under way while the lengths say which hold a part (loads of the others are
 // of memory that is the call's, and dropped).  Relaxed atomic loads are plain ones that the compiler leaves in their
-// place: others it moves behind the branches that the lengths decide (25 places of 32 rows: 5.3 -> 4.0 us).
+// place: others it moves behind the branches that decide (medians: 25 places of 32 rows 3.6 -> 3.2 us, 4 of 16384 rows 8.3 -> 7.5;
+// no difference where the lengths of shared rows decide, as their loads take longer than these).
 template <int DT, int D, int MODE, int N>
 __global__ void __launch_bounds__(256) places_join_kernel(ArgsOf<MODE> a) {
   constexpr int EPL = D / 64;
