@@ -652,7 +652,8 @@ typedef struct {
  * read for all its sequences together.
  * Workspace: dc_shared_workspace_bytes(dims, tokens, shared, kv->len + max_tokens) bytes, as for
  * dc_prompt_attention the call's alone until it has run.  It holds the parts of a row's keys, 2 to 64 times the outputs in
- * float32 by the number of tokens; prompts that fill the card twice with whole tiles of 128 (token, head) rows take none.
+ * float32 by the number of tokens; prompts that fill the card twice with whole tiles of 128 (token, head) rows, or eight times
+ * with tiles full to 98 %, take none.
  * out overlaps nothing that the call reads, the prefixes' cache among it.
  * Errors: those of dc_prompt_attention, dc_tree_attention; DC_ERR_NULL (shared, its cache), DC_ERR_SHAPE (its
  * sizes), DC_ERR_UNSUPPORTED (its alignment, overlaps, more than 2^24 units). */
